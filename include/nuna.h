@@ -413,6 +413,160 @@ nuna_status_t nuna_all_to_all_combine(const void* const* y, void* const* out, co
                                       nuna_dtype_t dtype, nuna_placement_t place, hipStream_t stream);
 
 /*
+ * The rank-local half of an expert layer: what a rank does between the
+ * dispatch that brings its token rows and the combine that takes the results
+ * back.  The rows are put into the order of the experts, multiplied by the
+ * experts' weights in 8-bit floating point, and brought back, weighted.
+ *
+ * Common rules.  All pointers are DEVICE memory (tables 4-byte, everything
+ * else 16-byte aligned); every call enqueues on `stream`, allocates nothing,
+ * does not synchronise and can be captured.  Indices read from device memory
+ * (rows, slots, offsets) are checked there: an index outside its buffer is
+ * skipped, or cut to the buffer.  Outputs must not overlap inputs
+ * (NUNA_ERR_OVERLAP).  Sums are held in fp32; results do not depend on timing
+ * (no floating-point atomics).  Sizes of zero are valid and launch nothing
+ * where there is nothing to write.
+ */
+
+/* Largest number of experts (groups) a call takes. */
+#define NUNA_MAX_EXPERTS 1024
+
+/*
+ * Slots sorted by expert (stable).  A slot is one entry of the top-k table,
+ * slot t * topk + j being choice j of token t; it is local when its expert is
+ * in [first_expert, first_expert + num_experts), and other slots (other
+ * ranks' experts, or negative numbers for choices that were dropped) are
+ * ordinary input that sorts nowhere.
+ *   topk_idx  int32 [tokens][topk]
+ *   offsets   int32 [num_experts + 1], written: local expert e holds the rows
+ *             [offsets[e], offsets[e + 1]) of the order
+ *   slot_of   int32 [tokens * topk], written: the slot of each row, ascending
+ *             within an expert; -1 past the last row
+ *   row_of    int32 [tokens][topk], written: the row of each slot, or -1
+ *   workspace nuna_moe_sort_workspace bytes (0: may be NULL); its contents
+ *             need not be kept or cleared between calls
+ * tokens * topk <= 2^30; 1 <= topk <= NUNA_MAX_EXPERTS; 1 <= num_experts <=
+ * NUNA_MAX_EXPERTS.
+ */
+nuna_status_t nuna_moe_sort_workspace(int64_t tokens, int topk, int num_experts, size_t* bytes);
+nuna_status_t nuna_moe_sort(const int32_t* topk_idx, int64_t tokens, int topk, int first_expert, int num_experts,
+                            int32_t* offsets, int32_t* slot_of, int32_t* row_of, void* workspace,
+                            size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Rows into expert order: y[row_of[t][j], :] = x[t, :] for every slot with a
+ * row in [0, capacity_rows).  Rows of y that no slot names are left untouched.
+ *   x  [tokens][x_stride >= row_elems] of dtype;  y  [capacity_rows][row_elems]
+ * Its gradient is nuna_moe_scatter with weights NULL.
+ *
+ * nuna_moe_gather_f8 quantises each row on the way, once, as
+ * nuna_f8_quantize does: y is [capacity_rows][kp] and y_scale
+ * [capacity_rows][pitch], kp and pitch as given there for cols = row_elems.
+ */
+typedef enum { NUNA_SCALE_F32 = 0, NUNA_SCALE_E8M0 = 1 } nuna_scale_t;
+nuna_status_t nuna_moe_gather(const void* x, int64_t x_stride, const int32_t* row_of, int64_t tokens, int topk,
+                              size_t row_elems, void* y, size_t capacity_rows, nuna_dtype_t dtype,
+                              hipStream_t stream);
+nuna_status_t nuna_moe_gather_f8(const void* x, int64_t x_stride, const int32_t* row_of, int64_t tokens, int topk,
+                                 size_t row_elems, void* y, void* y_scale, size_t capacity_rows,
+                                 nuna_dtype_t dtype, nuna_scale_t scale, hipStream_t stream);
+
+/*
+ * Rows back to their tokens:
+ *   out[t, :] = sum over j of weights[t][j] * y[row_of[t][j], :]
+ * over the slots with a row in [0, capacity_rows), j ascending, in fp32 (one
+ * fused multiply-add a term, or an add where weights is NULL) with one
+ * rounding to dtype.  A token without a row gets zeros; every row of out is
+ * written.
+ *   y  [capacity_rows][row_elems];  weights  fp32 [tokens][topk] or NULL;
+ *   out  [tokens][row_elems]
+ *
+ * nuna_moe_scatter_grad is its gradient: for those slots
+ *   dy[row_of[t][j], :] = weights[t][j] * dout[t, :]          (rounded once)
+ *   dweights[t][j] = sum over c of dout[t, c] * y[row_of[t][j], c]   (fp32)
+ * and dweights of every other slot is 0; other rows of dy are left untouched.
+ */
+nuna_status_t nuna_moe_scatter(const void* y, const int32_t* row_of, const float* weights, int64_t tokens, int topk,
+                               size_t row_elems, size_t capacity_rows, void* out, nuna_dtype_t dtype,
+                               hipStream_t stream);
+nuna_status_t nuna_moe_scatter_grad(const void* dout, const void* y, const int32_t* row_of, const float* weights,
+                                    int64_t tokens, int topk, size_t row_elems, size_t capacity_rows, void* dy,
+                                    float* dweights, nuna_dtype_t dtype, hipStream_t stream);
+
+/*
+ * 8-bit matrices.  A matrix of `cols` columns is kept as e4m3 bytes (the OCP
+ * format: largest value 448, no infinities) in rows of kp = cols rounded up
+ * to a multiple of NUNA_F8_BLOCK, zeros past the last column, with a scale
+ * for each block of NUNA_F8_BLOCK columns: value = byte * scale.  A row of
+ * scales has pitch = kp / NUNA_F8_BLOCK rounded up to a multiple of 4
+ * entries; the entries past the last block are written as 1 and not read.
+ * Scales are fp32 (NUNA_SCALE_F32) or powers of two in one byte
+ * (NUNA_SCALE_E8M0: 2^(byte - 127), 255 a NaN), which the matrix
+ * instructions apply themselves.
+ *
+ * Quantising a block with largest magnitude m:
+ *   s = max(m / 448, 2^-126) in fp32; NaN if m is not finite;
+ *   NUNA_SCALE_E8M0: s is rounded up to a power of two;
+ *   byte = e4m3(x * (1 / s)), rounded to nearest even.
+ *
+ * nuna_f8_quantize: x [rows][x_stride >= cols]; blocks of 1 x 128.
+ *   out [rows][kp], scale [rows][pitch]
+ * nuna_f8_quantize_blocks: x [batch][rows][cols]; blocks of 128 x 128
+ *   (weights: their transpose has the transposed scales).
+ *   out [batch][rows][kp], scale [batch][ceil(rows / 128)][pitch]
+ * nuna_f8_quantize_cols: x [x_rows][x_stride >= cols]; blocks of 128 x 1
+ *   along the rows of each group, written transposed, as nuna_f8_wgrad reads
+ *   them.  Row r of group g (offsets[g] <= r < offsets[g + 1], r < rows) is row r
+ *   of x, or with slot_of row slot_of[r] / topk (a negative slot: zeros).  It
+ *   becomes column 128 * (offsets[g] / 128 + g) + r - offsets[g], so every
+ *   group starts at a block of its own.
+ *   offsets int32 [groups + 1] ascending from 0; slot_of int32 [rows] or NULL
+ *   (then rows <= x_rows); out [cols][tc], tc = 128 * (rows / 128 + groups),
+ *   scale [cols][pitch of tc].  Columns and blocks that hold no row are
+ *   written as zeros.
+ */
+#define NUNA_F8_BLOCK 128
+nuna_status_t nuna_f8_quantize(const void* x, int64_t x_stride, size_t rows, size_t cols, nuna_dtype_t dtype,
+                               void* out, void* scale, nuna_scale_t kind, hipStream_t stream);
+nuna_status_t nuna_f8_quantize_blocks(const void* x, int batch, size_t rows, size_t cols, nuna_dtype_t dtype,
+                                      void* out, void* scale, nuna_scale_t kind, hipStream_t stream);
+nuna_status_t nuna_f8_quantize_cols(const void* x, int64_t x_stride, size_t x_rows, const int32_t* slot_of, int topk,
+                                    const int32_t* offsets, int groups, size_t rows, size_t cols,
+                                    nuna_dtype_t dtype, void* out, void* scale, nuna_scale_t kind,
+                                    hipStream_t stream);
+
+/*
+ * Products of 8-bit matrices.
+ *
+ * nuna_f8_matmul: out[r, c] = sum over i of a[r, i] * b[g][c, i], with g the
+ * group of row r.
+ *   a        [rows][k] with a_scale [rows][pitch]
+ *   b        [groups][n][k] with b_scale [groups][ceil(n / 128)][pitch]
+ *   offsets  int32 [groups + 1] ascending, as nuna_moe_sort writes them: group
+ *            g holds the rows [offsets[g], offsets[g + 1]); rows that no group
+ *            holds are left untouched.  NULL: one group of all rows (groups
+ *            must be 1).
+ *   out      [rows][n] of out_dtype
+ * The gradient of a is the same call on the transposed weights.
+ *
+ * nuna_f8_wgrad: out[g][i, j] = sum over the rows r of group g of
+ * a[i, r] * b[j, r], the gradient of the weights.  Both operands as
+ * nuna_f8_quantize_cols writes them for `rows` rows and these offsets:
+ *   a  [n][tc] with its scales;  b  [k][tc] with its scales;
+ *   out  [groups][n][k] of out_dtype; a group without rows gets zeros.
+ *
+ * k of nuna_f8_matmul is a multiple of NUNA_F8_BLOCK (NUNA_ERR_UNSUPPORTED
+ * otherwise), n any.  Each block of 128 is summed by the matrix instructions
+ * in fp32; fp32 scales multiply the block's sum.
+ */
+nuna_status_t nuna_f8_matmul(const void* a, const void* a_scale, const void* b, const void* b_scale,
+                             const int32_t* offsets, int groups, size_t rows, size_t n, size_t k, void* out,
+                             nuna_scale_t kind, nuna_dtype_t out_dtype, hipStream_t stream);
+nuna_status_t nuna_f8_wgrad(const void* a, const void* a_scale, const void* b, const void* b_scale,
+                            const int32_t* offsets, int groups, size_t rows, size_t n, size_t k, void* out,
+                            nuna_scale_t kind, nuna_dtype_t out_dtype, hipStream_t stream);
+
+/*
  * NUNA-aware placement planner: Algorithm 1 of the paper (Sec. 4.2.2,
  * logical allocation then physical placement), host-only, no HIP call.
  *

@@ -20,6 +20,7 @@
 #include <vector>
 
 #include "a2a_order.h"
+#include "api_common.h"
 #include "fastdiv.h"
 #include "kernels.h"
 #include "nap_planner.h"
@@ -212,6 +213,19 @@ const TunableDef* find_tunable(const char* name) {
 }  // namespace
 
 namespace nuna {
+nuna_status_t api_fail(nuna_status_t st, const char* fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    std::vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    return fail(st, "%s", buf);
+}
+nuna_status_t api_ok() { return ok(); }
+nuna_status_t api_exception() { return host_exception(); }
+nuna_status_t api_hip(hipError_t e, const char* what) { return hip_status(e, what); }
+void api_begin_launches() { begin_launches(); }
+
 int64_t combine_copies() { return t_combine_copies; }
 
 void note_launch(const char* kernel, int map, int64_t group_size, int64_t grid, int threads, int vpt) {

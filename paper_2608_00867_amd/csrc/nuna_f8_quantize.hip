@@ -1,0 +1,281 @@
+// nuna_f8_quantize.hip -- rows, weight blocks and columns to e4m3 with a scale
+// for each block of 128 (the rule is in f8_common.h).
+//
+// All three read each value once and write one byte for it, and are bound by
+// HBM.  A thread holds its values in registers between the block's largest
+// magnitude and the rounding, so nothing is read twice.
+#include <algorithm>
+
+#include "f8_common.h"
+
+namespace nuna {
+namespace {
+
+// Sixteen consecutive values of a row of which the first `n` exist, widened; zeros past them.
+template <int DT>
+__device__ __forceinline__ void load_values(const char* p, int64_t n, float (&v)[16]) {
+    constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
+    if (n >= 16) {
+        uint4 raw[16 / L];
+#pragma unroll
+        for (int i = 0; i < 16 / L; ++i) raw[i] = load16_any(p + i * 16);
+#pragma unroll
+        for (int i = 0; i < 16 / L; ++i) Arith<DT>::init(reinterpret_cast<float(&)[L]>(v[i * L]), raw[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            v[i] = i < n ? Arith<DT>::widen1(*reinterpret_cast<const typename Arith<DT>::Raw*>(p + i * ES)) : 0.0f;
+    }
+}
+
+__device__ __forceinline__ uint32_t max_abs(const float (&v)[16]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max(m, abs_bits(v[i]));
+    return m;
+}
+
+__device__ __forceinline__ uint4 to_e4m3x16(const float (&v)[16], float r) {
+    uint32_t q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = to_e4m3x4(v[4 * i] * r, v[4 * i + 1] * r, v[4 * i + 2] * r, v[4 * i + 3] * r);
+    return make_uint4(q[0], q[1], q[2], q[3]);
+}
+
+// ---------------------------------------------------------------- rows
+
+constexpr int kRowsPerWave = 8;  // blocks of 128 columns a wave quantises, 8 lanes each, 16 values a lane
+
+// Work item, one a wave: kRowsPerWave blocks of one row.  GATHER: the row goes to the topk rows that row_of names.
+template <int DT, int KIND, bool GATHER>
+__global__ __launch_bounds__(kWG) void k_f8_rows(const char* __restrict__ x, int64_t x_stride,
+                                                 const int32_t* __restrict__ row_of, int topk, int64_t cols,
+                                                 int64_t blocks, int64_t pitch, int chunks, int64_t items, int64_t cap,
+                                                 uint8_t* __restrict__ out, void* __restrict__ scale) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t wg = blockIdx.x; wg * (kWG / 64) < items; wg += gridDim.x) {
+        const int64_t item = wg * (kWG / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (item >= items) continue;
+        const int64_t row = item / chunks;
+        const int64_t block = (item - row * chunks) * kRowsPerWave + (lane >> 3);
+        if (block >= pitch) continue;
+        uint4 q = make_uint4(0, 0, 0, 0);
+        uint32_t kept = kScaleOne<KIND>;
+        if (block < blocks) {
+            const int64_t c = block * kF8Block + (lane & 7) * 16;
+            float v[16];
+            load_values<DT>(x + (row * x_stride + c) * Arith<DT>::kEsize, cols - c, v);
+            const BlockScale s = block_scale<KIND>(max_oct(max_abs(v)));
+            q = to_e4m3x16(v, s.r);
+            kept = s.kept;
+        }
+        const auto put = [&](int64_t to) {
+            if (block < blocks)
+                *reinterpret_cast<uint4*>(out + (to * blocks + block) * kF8Block + (lane & 7) * 16) = q;
+            if ((lane & 7) == 0) store_scale<KIND>(scale, to * pitch + block, kept);
+        };
+        if constexpr (GATHER) {
+            for (int j = 0; j < topk; ++j) {
+                const int to = row_of[row * topk + j];
+                if (to >= 0 && to < cap) put(to);
+            }
+        } else {
+            put(row);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- blocks
+
+// Work item: one block of 128 x 128.  Thread t holds 16 columns of the rows t / 8 + 32 i.
+template <int DT, int KIND>
+__global__ __launch_bounds__(kWG) void k_f8_blocks(const char* __restrict__ x, int64_t rows, int64_t cols,
+                                                   int64_t row_blocks, int64_t blocks, int64_t pitch, int64_t items,
+                                                   uint8_t* __restrict__ out, void* __restrict__ scale) {
+    __shared__ uint32_t wave_max[kWG / 64];
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t cb = item % blocks, rb = item / blocks % row_blocks, batch = item / (blocks * row_blocks);
+        const int64_t c = cb * kF8Block + (threadIdx.x & 7) * 16;
+        float v[4][16];
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t r = rb * kF8Block + (threadIdx.x >> 3) + 32 * i;
+            load_values<DT>(x + ((batch * rows + r) * cols + c) * Arith<DT>::kEsize, r < rows ? cols - c : 0, v[i]);
+            m = max(m, max_abs(v[i]));
+        }
+        for (int d = 32; d > 0; d >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), d)));
+        if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = m;
+        __syncthreads();
+        for (int w = 0; w < kWG / 64; ++w) m = max(m, wave_max[w]);
+        __syncthreads();
+        const BlockScale s = block_scale<KIND>(m);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t r = rb * kF8Block + (threadIdx.x >> 3) + 32 * i;
+            if (r < rows) *reinterpret_cast<uint4*>(out + (batch * rows + r) * blocks * kF8Block + c) = to_e4m3x16(v[i], s.r);
+        }
+        const int64_t at = (batch * row_blocks + rb) * pitch;
+        if (threadIdx.x == 0) store_scale<KIND>(scale, at + cb, s.kept);
+        if (cb == blocks - 1 && threadIdx.x < pitch - blocks)
+            store_scale<KIND>(scale, at + blocks + threadIdx.x, kScaleOne<KIND>);
+    }
+}
+
+// ---------------------------------------------------------------- columns
+
+// Work item: 64 dwords of columns (128 of bf16, 64 of fp32) of the 128 rows of one block of a group.  The rows go to
+// LDS as they lie, then thread (c, q) takes the column dword c of the rows 32 q .. 32 q + 31.  Row r's dwords are
+// turned by 16 (r / 32), so the four quarters of a column, which neighbouring lanes read, lie in other banks.
+template <int DT, int KIND>
+__global__ __launch_bounds__(kWG) void k_f8_cols(const char* __restrict__ x, int64_t x_stride, int64_t x_rows,
+                                                 const int32_t* __restrict__ slot_of, int topk,
+                                                 const int32_t* __restrict__ offsets, int groups, int64_t rows,
+                                                 int64_t cols, int64_t blocks, int64_t pitch, int chunks, int64_t items,
+                                                 uint8_t* __restrict__ out, void* __restrict__ scale) {
+    constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
+    constexpr int kPer = 4 / ES;             // columns of a dword
+    constexpr int kCols = 64 * kPer;         // columns of a work item
+    __shared__ __align__(16) uint32_t tile[kF8Block * 64];
+    const int tid = threadIdx.x, lane = tid & 63;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t block = item / chunks;
+        const int64_t c0 = (item - block * chunks) * kCols;
+        // The group of this block: the last whose first block is not past it.
+        int g = -1;
+        for (int i = 0; i < groups; i += 64) {
+            const bool upto = i + lane < groups && group_offset(offsets, i + lane, rows) / kF8Block + i + lane <= block;
+            g += __popcll(__ballot(upto));
+        }
+        int64_t row0 = 0, count = 0;
+        if (g >= 0) {
+            const int64_t from = group_offset(offsets, g, rows), to = group_offset(offsets, g + 1, rows);
+            row0 = from + (block - (from / kF8Block + g)) * kF8Block;
+            count = to - row0;
+        }
+        // 16 threads a row, 16 rows a pass.
+        const int64_t c = c0 + (tid & 15) * L;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = (tid >> 4) + 16 * i;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (r < count && c < cols) {
+                int64_t from = row0 + r;
+                if (slot_of) {
+                    const int slot = slot_of[from];
+                    from = slot < 0 || slot / topk >= x_rows ? -1 : slot / topk;
+                }
+                if (from >= 0) {
+                    const char* p = x + (from * x_stride + c) * ES;
+                    if (c + L <= cols) {
+                        v = load16_any(p);
+                    } else {
+                        typename Arith<DT>::Raw part[L] = {};
+                        for (int k = 0; c + k < cols; ++k) part[k] = reinterpret_cast<const typename Arith<DT>::Raw*>(p)[k];
+                        v = __builtin_bit_cast(uint4, part);
+                    }
+                }
+            }
+            *reinterpret_cast<uint4*>(&tile[r * 64 + (((tid & 15) * 4 + 16 * (r >> 5)) & 63)]) = v;
+        }
+        __syncthreads();
+        const int q = lane & 3, cd = (tid >> 6) * 16 + (lane >> 2);
+        uint32_t w[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) w[i] = tile[(q * 32 + i) * 64 + ((cd + 16 * q) & 63)];
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < kPer; ++h) {
+            const auto value = [&](int i) {
+                return kPer == 1 ? __uint_as_float(w[i]) : h == 0 ? bf16_lo(w[i]) : bf16_hi(w[i]);
+            };
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) m = max(m, abs_bits(value(i)));
+            const BlockScale s = block_scale<KIND>(max_quad(m));
+            uint32_t b[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                b[i] = to_e4m3x4(value(4 * i) * s.r, value(4 * i + 1) * s.r, value(4 * i + 2) * s.r, value(4 * i + 3) * s.r);
+            const int64_t col = c0 + cd * kPer + h;
+            if (col < cols) {
+                uint4* to = reinterpret_cast<uint4*>(out + (col * blocks + block) * kF8Block + q * 32);
+                to[0] = make_uint4(b[0], b[1], b[2], b[3]);
+                to[1] = make_uint4(b[4], b[5], b[6], b[7]);
+                if (q == 0) store_scale<KIND>(scale, col * pitch + block, s.kept);
+                if (block == blocks - 1 && q < pitch - blocks)
+                    store_scale<KIND>(scale, col * pitch + blocks + q, kScaleOne<KIND>);
+            }
+        }
+    }
+}
+
+template <class F>
+void by_type(int dtype, int kind, F f) {
+    const auto typed = [&](auto dt) {
+        if (kind == kScaleF32)
+            f(dt, std::integral_constant<int, kScaleF32>{});
+        else
+            f(dt, std::integral_constant<int, kScaleE8m0>{});
+    };
+    if (dtype == kDtBf16)
+        typed(std::integral_constant<int, kDtBf16>{});
+    else
+        typed(std::integral_constant<int, kDtF32>{});
+}
+
+// One work item a workgroup up to 2^20 workgroups or the caller's cap; a loop beyond.
+int64_t quantize_grid(int64_t items) { return std::min(items, grid_limit(int64_t(1) << 20)); }
+
+}  // namespace
+
+hipError_t launch_f8_rows(const void* x, int64_t x_stride, const int32_t* row_of, int topk, int64_t rows, int64_t cols,
+                          int64_t cap, int dtype, void* out, void* scale, int kind, hipStream_t stream) {
+    const int64_t blocks = f8_width(cols) / kF8Block, pitch = f8_pitch(cols);
+    const int chunks = static_cast<int>((pitch + kRowsPerWave - 1) / kRowsPerWave);
+    const int64_t items = rows * chunks, grid = quantize_grid((items + kWG / 64 - 1) / (kWG / 64));
+    by_type(dtype, kind, [&](auto dt, auto k) {
+        constexpr int DT = decltype(dt)::value, KIND = decltype(k)::value;
+        if (row_of)
+            k_f8_rows<DT, KIND, true><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(
+                static_cast<const char*>(x), x_stride, row_of, topk, cols, blocks, pitch, chunks, items, cap,
+                static_cast<uint8_t*>(out), scale);
+        else
+            k_f8_rows<DT, KIND, false><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(
+                static_cast<const char*>(x), x_stride, nullptr, 0, cols, blocks, pitch, chunks, items, cap,
+                static_cast<uint8_t*>(out), scale);
+    });
+    note_launch(row_of ? "k_f8_rows_gather" : "k_f8_rows", kMapLinear, 1, grid, kWG, 1);
+    return hipGetLastError();
+}
+
+hipError_t launch_f8_blocks(const void* x, int64_t batch, int64_t rows, int64_t cols, int dtype, void* out, void* scale,
+                            int kind, hipStream_t stream) {
+    const int64_t blocks = f8_width(cols) / kF8Block, pitch = f8_pitch(cols);
+    const int64_t row_blocks = (rows + kF8Block - 1) / kF8Block;
+    const int64_t items = batch * row_blocks * blocks, grid = quantize_grid(items);
+    by_type(dtype, kind, [&](auto dt, auto k) {
+        k_f8_blocks<decltype(dt)::value, decltype(k)::value><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(
+            static_cast<const char*>(x), rows, cols, row_blocks, blocks, pitch, items, static_cast<uint8_t*>(out), scale);
+    });
+    note_launch("k_f8_blocks", kMapLinear, 1, grid, kWG, 1);
+    return hipGetLastError();
+}
+
+hipError_t launch_f8_cols(const void* x, int64_t x_stride, int64_t x_rows, const int32_t* slot_of, int topk,
+                          const int32_t* offsets, int groups, int64_t rows, int64_t cols, int dtype, void* out,
+                          void* scale, int kind, hipStream_t stream) {
+    const int64_t width = f8_t_width(rows, groups), blocks = width / kF8Block, pitch = f8_pitch(width);
+    const int per = dtype == kDtBf16 ? 128 : 64;
+    const int chunks = static_cast<int>((cols + per - 1) / per);
+    const int64_t items = blocks * chunks, grid = quantize_grid(items);
+    by_type(dtype, kind, [&](auto dt, auto k) {
+        k_f8_cols<decltype(dt)::value, decltype(k)::value><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(
+            static_cast<const char*>(x), x_stride, x_rows, slot_of, topk, offsets, groups, rows, cols, blocks, pitch,
+            chunks, items, static_cast<uint8_t*>(out), scale);
+    });
+    note_launch("k_f8_cols", kMapLinear, 1, grid, kWG, 1);
+    return hipGetLastError();
+}
+
+}  // namespace nuna

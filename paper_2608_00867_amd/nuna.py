@@ -22,6 +22,9 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_MISALIGNED, ERR_OVERLAP, ERR_HIP, ERR_
 STATUS_NAMES = {0: "NUNA_OK", 1: "NUNA_ERR_INVALID_ARG", 2: "NUNA_ERR_UNSUPPORTED", 3: "NUNA_ERR_MISALIGNED",
                 4: "NUNA_ERR_OVERLAP", 5: "NUNA_ERR_HIP", 6: "NUNA_ERR_NO_MEMORY"}
 F32, BF16 = 0, 1
+SCALE_F32, SCALE_E8M0 = 0, 1
+F8_BLOCK = 128
+MAX_EXPERTS = 1024
 LINEAR, XCD = 0, 1
 ALGO_AUTO, ALGO_ONE_SHOT, ALGO_TWO_SHOT, ALGO_ONE_SHOT_SPLIT, ALGO_TWO_SHOT_TWO_KERNELS = 0, 1, 2, 3, 4
 
@@ -91,6 +94,29 @@ SIGNATURES = {
                                 ctypes.c_size_t, ctypes.c_size_t, ctypes.c_int, ctypes.c_int, _vp, _vp], ctypes.c_int),
     "nuna_all_to_all_combine": ([_vpp, _vpp, _vp, _vp, ctypes.c_size_t, ctypes.c_size_t, ctypes.c_int,
                                  ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_moe_sort_workspace": ([ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)],
+                                ctypes.c_int),
+    "nuna_moe_sort": ([_vp, ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, _vp,
+                       ctypes.c_size_t, _vp], ctypes.c_int),
+    "nuna_moe_gather": ([_vp, ctypes.c_int64, _vp, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, _vp, ctypes.c_size_t,
+                         ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_moe_gather_f8": ([_vp, ctypes.c_int64, _vp, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, _vp, _vp,
+                            ctypes.c_size_t, ctypes.c_int, ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_moe_scatter": ([_vp, _vp, _vp, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, ctypes.c_size_t, _vp,
+                          ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_moe_scatter_grad": ([_vp, _vp, _vp, _vp, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, ctypes.c_size_t, _vp,
+                               _vp, ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_f8_quantize": ([_vp, ctypes.c_int64, ctypes.c_size_t, ctypes.c_size_t, ctypes.c_int, _vp, _vp, ctypes.c_int,
+                          _vp], ctypes.c_int),
+    "nuna_f8_quantize_blocks": ([_vp, ctypes.c_int, ctypes.c_size_t, ctypes.c_size_t, ctypes.c_int, _vp, _vp,
+                                 ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_f8_quantize_cols": ([_vp, ctypes.c_int64, ctypes.c_size_t, _vp, ctypes.c_int, _vp, ctypes.c_int,
+                               ctypes.c_size_t, ctypes.c_size_t, ctypes.c_int, _vp, _vp, ctypes.c_int, _vp],
+                              ctypes.c_int),
+    "nuna_f8_matmul": ([_vp, _vp, _vp, _vp, _vp, ctypes.c_int, ctypes.c_size_t, ctypes.c_size_t, ctypes.c_size_t, _vp,
+                        ctypes.c_int, ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_f8_wgrad": ([_vp, _vp, _vp, _vp, _vp, ctypes.c_int, ctypes.c_size_t, ctypes.c_size_t, ctypes.c_size_t, _vp,
+                       ctypes.c_int, ctypes.c_int, _vp], ctypes.c_int),
     "nuna_placement_items": ([ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, _i64p,
                               ctypes.c_int64, _i64p], ctypes.c_int),
     "nuna_placement_grid": ([ctypes.c_int, ctypes.c_int64, ctypes.c_int64, _i64p], ctypes.c_int),
@@ -550,6 +576,303 @@ def all_to_all_combine(y, out, layout, placement="xcd", stream=None, weights=Non
         cap = min(cap, t.shape[0])
     _check(all_to_all_combine_raw([t.data_ptr() for t in y], [t.data_ptr() for t in out], layout.handle, row, cap,
                                   _dtype_code(out[0]), PLACEMENTS[placement], _stream(stream), wp))
+    return out
+
+
+# ------------------------------------------------------------------ the expert layer
+
+SCALES = {"f32": SCALE_F32, "e8m0": SCALE_E8M0}
+
+
+def f8_width(cols):
+    """Columns of an 8-bit matrix as it is kept: whole blocks of 128."""
+    return -(-cols // F8_BLOCK) * F8_BLOCK
+
+
+def f8_pitch(cols):
+    """Scales in one of its rows: a block each, to a multiple of four."""
+    return -(-(f8_width(cols) // F8_BLOCK) // 4) * 4
+
+
+def f8_cols_width(rows, groups):
+    """Columns of `rows` rows laid out along the rows of `groups` groups (f8_quantize_cols)."""
+    return F8_BLOCK * (rows // F8_BLOCK + groups)
+
+
+def _scale_kind(t, name="scale"):
+    torch = _torch()
+    if t.dtype == torch.float32:
+        return SCALE_F32
+    if t.dtype == torch.float8_e8m0fnu:
+        return SCALE_E8M0
+    raise TypeError(f"{name}: unsupported scale dtype {t.dtype}")
+
+
+def _scale_dtype(scale):
+    torch = _torch()
+    if scale not in SCALES:
+        raise ValueError(f"scale {scale!r} is not one of {sorted(SCALES)}")
+    return torch.float32 if scale == "f32" else torch.float8_e8m0fnu
+
+
+def _check_tensor(t, name, shape, dtype):
+    """A contiguous CUDA tensor of this shape and dtype."""
+    if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a contiguous CUDA tensor {list(shape)} of {dtype}, "
+                         f"got {list(t.shape)} of {t.dtype}")
+
+
+def _check_matrix(t, name):
+    """A CUDA tensor [rows, cols] whose rows are contiguous; returns its row stride."""
+    if not t.is_cuda or t.dim() != 2 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a CUDA tensor [rows, cols] with contiguous rows")
+    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if stride < t.shape[1]:
+        raise ValueError(f"{name}: its rows overlap")
+    return stride
+
+
+def _check_table(t, name):
+    if not t.is_cuda or not t.is_contiguous() or t.dim() != 2 or t.dtype != _torch().int32 or t.shape[1] < 1:
+        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor [tokens, topk]")
+    return int(t.shape[0]), int(t.shape[1])
+
+
+def _check_offsets(t):
+    if not t.is_cuda or not t.is_contiguous() or t.dim() != 1 or t.dtype != _torch().int32 or t.numel() < 2:
+        raise ValueError("offsets must be a contiguous int32 CUDA tensor [groups + 1]")
+    return t.numel() - 1
+
+
+def _new(stream, shape, dtype, device):
+    """An uninitialised tensor that belongs to the stream it is used on."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if isinstance(stream, int):
+        raise ValueError("a raw stream handle needs every output and workspace to be given")
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _f8_outputs(out, scale_out, shape, scale_shape, scale, stream, device):
+    """The 8-bit output and its scales: those given, checked, or new ones of the scale type `scale`."""
+    torch = _torch()
+    if out is None:
+        out = _new(stream, shape, torch.float8_e4m3fn, device)
+    if scale_out is None:
+        scale_out = _new(stream, scale_shape, _scale_dtype(scale), device)
+    _check_tensor(out, "out", shape, torch.float8_e4m3fn)
+    _check_tensor(scale_out, "scale_out", scale_shape, _scale_dtype(scale))
+    return out, scale_out
+
+
+def moe_sort_workspace(tokens, topk, num_experts):
+    """Bytes of workspace that moe_sort needs."""
+    n = ctypes.c_size_t()
+    _check(lib().nuna_moe_sort_workspace(int(tokens), int(topk), int(num_experts), ctypes.byref(n)))
+    return n.value
+
+
+def moe_sort(topk_idx, num_experts, first_expert=0, offsets=None, slot_of=None, row_of=None, workspace=None,
+             stream=None):
+    """Sort the slots of topk_idx (int32 CUDA tensor [T, k]) by expert, stable, for the num_experts experts from
+    first_expert on; other entries sort nowhere.  Returns (offsets [num_experts + 1], slot_of [T * k], row_of [T, k]),
+    int32: expert e holds the rows offsets[e] .. offsets[e + 1], slot_of[row] is a row's slot t * k + j (-1 past the
+    last), row_of[t, j] a slot's row (-1: none).  workspace: a uint8 CUDA tensor of moe_sort_workspace bytes."""
+    torch = _torch()
+    T, k = _check_table(topk_idx, "topk_idx")
+    num_experts = int(num_experts)
+    need = moe_sort_workspace(T, k, num_experts)
+    dev = topk_idx.device
+    offsets = _new(stream, (num_experts + 1,), torch.int32, dev) if offsets is None else offsets
+    slot_of = _new(stream, (T * k,), torch.int32, dev) if slot_of is None else slot_of
+    row_of = _new(stream, (T, k), torch.int32, dev) if row_of is None else row_of
+    _check_tensor(offsets, "offsets", (num_experts + 1,), torch.int32)
+    _check_tensor(slot_of, "slot_of", (T * k,), torch.int32)
+    _check_tensor(row_of, "row_of", (T, k), torch.int32)
+    if workspace is None:
+        workspace = _new(stream, (need,), torch.uint8, dev) if need else None
+    elif not workspace.is_cuda or not workspace.is_contiguous() or workspace.dtype != torch.uint8:
+        raise ValueError("workspace must be a contiguous uint8 CUDA tensor")
+    _check(lib().nuna_moe_sort(topk_idx.data_ptr(), T, k, int(first_expert), num_experts, offsets.data_ptr(),
+                               slot_of.data_ptr(), row_of.data_ptr(), workspace.data_ptr() if need else None,
+                               workspace.numel() if need else 0, _stream(stream)))
+    return offsets, slot_of, row_of
+
+
+def moe_gather(x, row_of, out, scale_out=None, stream=None):
+    """out[row_of[t, j]] = x[t] for every slot with a row of out; other rows are left untouched.  x [T, H] with
+    contiguous rows.  out [rows, H] of x's dtype, or float8_e4m3fn [rows, f8_width(H)] with scale_out [rows,
+    f8_pitch(H)] (float32 or float8_e8m0fnu): each row quantised as f8_quantize does.  Returns out, or (out,
+    scale_out).  The gradient of the first form is moe_scatter without weights."""
+    torch = _torch()
+    T, k = _check_table(row_of, "row_of")
+    stride = _check_matrix(x, "x")
+    H = x.shape[1]
+    if x.shape[0] != T:
+        raise ValueError(f"x has {x.shape[0]} rows, row_of {T}")
+    if out.dim() != 2:
+        raise ValueError("out must be [rows, columns]")
+    cap = out.shape[0]
+    if scale_out is None:
+        _check_tensor(out, "out", (cap, H), x.dtype)
+        _check(lib().nuna_moe_gather(x.data_ptr(), stride, row_of.data_ptr(), T, k, H, out.data_ptr(), cap,
+                                     _dtype_code(x), _stream(stream)))
+        return out
+    _check_tensor(out, "out", (cap, f8_width(H)), torch.float8_e4m3fn)
+    kind = _scale_kind(scale_out, "scale_out")
+    _check_tensor(scale_out, "scale_out", (cap, f8_pitch(H)), scale_out.dtype)
+    _check(lib().nuna_moe_gather_f8(x.data_ptr(), stride, row_of.data_ptr(), T, k, H, out.data_ptr(),
+                                    scale_out.data_ptr(), cap, _dtype_code(x), kind, _stream(stream)))
+    return out, scale_out
+
+
+def _check_weights(weights, T, k):
+    _check_tensor(weights, "weights", (T, k), _torch().float32)
+    return weights.data_ptr()
+
+
+def moe_scatter(y, row_of, weights=None, out=None, stream=None):
+    """out[t] = sum over j, ascending, of weights[t, j] * y[row_of[t, j]] (float32 weights [T, k], or None: 1) over
+    the slots with a row of y; fp32 sums, rounded once.  A token without a row gets zeros."""
+    T, k = _check_table(row_of, "row_of")
+    if y.dim() != 2:
+        raise ValueError("y must be [rows, columns]")
+    cap, H = y.shape
+    _check_tensor(y, "y", (cap, H), y.dtype)
+    wp = None if weights is None else _check_weights(weights, T, k)
+    if out is None:
+        out = _new(stream, (T, H), y.dtype, y.device)
+    _check_tensor(out, "out", (T, H), y.dtype)
+    _check(lib().nuna_moe_scatter(y.data_ptr(), row_of.data_ptr(), wp, T, k, H, cap, out.data_ptr(), _dtype_code(y),
+                                  _stream(stream)))
+    return out
+
+
+def moe_scatter_grad(dout, y, row_of, weights, dy=None, dweights=None, stream=None):
+    """Gradient of moe_scatter: (dy, dweights) with dy[row_of[t, j]] = weights[t, j] * dout[t] and dweights[t, j] =
+    <dout[t], y[row_of[t, j]]> (fp32; 0 for a slot without a row).  Rows of dy that no slot names are left untouched,
+    and are zeros where dy is not given."""
+    torch = _torch()
+    T, k = _check_table(row_of, "row_of")
+    if y.dim() != 2:
+        raise ValueError("y must be [rows, columns]")
+    cap, H = y.shape
+    _check_tensor(y, "y", (cap, H), y.dtype)
+    _check_tensor(dout, "dout", (T, H), y.dtype)
+    wp = _check_weights(weights, T, k)
+    if dy is None:
+        dy = _new(stream, (cap, H), y.dtype, y.device)
+        with torch.cuda.stream(stream):
+            dy.zero_()
+    if dweights is None:
+        dweights = _new(stream, (T, k), torch.float32, y.device)
+    _check_tensor(dy, "dy", (cap, H), y.dtype)
+    _check_tensor(dweights, "dweights", (T, k), torch.float32)
+    _check(lib().nuna_moe_scatter_grad(dout.data_ptr(), y.data_ptr(), row_of.data_ptr(), wp, T, k, H, cap,
+                                       dy.data_ptr(), dweights.data_ptr(), _dtype_code(y), _stream(stream)))
+    return dy, dweights
+
+
+def f8_quantize(x, scale="f32", out=None, scale_out=None, stream=None):
+    """x [rows, cols] (contiguous rows) to e4m3 with a scale ("f32" or "e8m0") for every 128 columns of a row.  Returns
+    (out float8_e4m3fn [rows, f8_width(cols)], zeros past the last column; scale_out [rows, f8_pitch(cols)])."""
+    stride = _check_matrix(x, "x")
+    rows, cols = x.shape
+    out, scale_out = _f8_outputs(out, scale_out, (rows, f8_width(cols)), (rows, f8_pitch(cols)), scale, stream,
+                                 x.device)
+    _check(lib().nuna_f8_quantize(x.data_ptr(), stride, rows, cols, _dtype_code(x), out.data_ptr(),
+                                  scale_out.data_ptr(), SCALES[scale], _stream(stream)))
+    return out, scale_out
+
+
+def f8_quantize_blocks(x, scale="f32", out=None, scale_out=None, stream=None):
+    """Weights x [.., rows, cols] to e4m3 with a scale for every block of 128 x 128.  Returns (out [.., rows,
+    f8_width(cols)], scale_out [.., ceil(rows / 128), f8_pitch(cols)])."""
+    if not x.is_cuda or not x.is_contiguous() or x.dim() < 2 or x.shape[-1] < 1:
+        raise ValueError("x must be a contiguous CUDA tensor [.., rows, cols]")
+    lead, (rows, cols) = tuple(x.shape[:-2]), x.shape[-2:]
+    batch = 1
+    for n in lead:
+        batch *= n
+    out, scale_out = _f8_outputs(out, scale_out, (*lead, rows, f8_width(cols)),
+                                 (*lead, -(-rows // F8_BLOCK), f8_pitch(cols)), scale, stream, x.device)
+    _check(lib().nuna_f8_quantize_blocks(x.data_ptr(), batch, rows, cols, _dtype_code(x), out.data_ptr(),
+                                         scale_out.data_ptr(), SCALES[scale], _stream(stream)))
+    return out, scale_out
+
+
+def f8_quantize_cols(x, offsets, scale="f32", out=None, scale_out=None, slot_of=None, topk=1, stream=None):
+    """The rows of x grouped by offsets (int32 [groups + 1]), transposed and quantised along the rows of each group: a
+    scale for every 128 rows of a group.  With slot_of (int32 [rows], of moe_sort) row r is row slot_of[r] // topk of
+    x, so that x need not be gathered first.  Returns (out [cols, f8_cols_width(rows, groups)], scale_out), the
+    operands of f8_wgrad."""
+    torch = _torch()
+    stride = _check_matrix(x, "x")
+    groups = _check_offsets(offsets)
+    x_rows, cols = x.shape
+    rows = x_rows
+    if slot_of is not None:
+        rows = slot_of.numel()
+        _check_tensor(slot_of, "slot_of", (rows,), torch.int32)
+    width = f8_cols_width(rows, groups)
+    out, scale_out = _f8_outputs(out, scale_out, (cols, width), (cols, f8_pitch(width)), scale, stream, x.device)
+    _check(lib().nuna_f8_quantize_cols(x.data_ptr(), stride, x_rows, None if slot_of is None else slot_of.data_ptr(),
+                                       int(topk), offsets.data_ptr(), groups, rows, cols, _dtype_code(x),
+                                       out.data_ptr(), scale_out.data_ptr(), SCALES[scale], _stream(stream)))
+    return out, scale_out
+
+
+def f8_matmul(a, a_scale, b, b_scale, out=None, offsets=None, out_dtype=None, stream=None):
+    """out[r] = b[g] @ a[r] in 8 bits, g the group of row r.  a [rows, k] with its scales (f8_quantize), b [groups, n,
+    k] with its block scales (f8_quantize_blocks); offsets int32 [groups + 1] (moe_sort); without offsets b is [n, k]
+    and every row is multiplied by it.  out [rows, n] of out_dtype (bfloat16 unless given); rows in no group are left
+    untouched."""
+    torch = _torch()
+    f8 = torch.float8_e4m3fn
+    groups = 1 if offsets is None else _check_offsets(offsets)
+    lead = () if offsets is None else (groups,)
+    if a.dim() != 2 or b.dim() != 2 + len(lead):
+        raise ValueError("a must be [rows, k] and b [n, k], or [groups, n, k] with offsets")
+    (rows, k), n = a.shape, b.shape[-2]
+    kind = _scale_kind(a_scale, "a_scale")
+    _check_tensor(a, "a", (rows, k), f8)
+    _check_tensor(b, "b", (*lead, n, k), f8)
+    _check_tensor(a_scale, "a_scale", (rows, f8_pitch(k)), a_scale.dtype)
+    _check_tensor(b_scale, "b_scale", (*lead, -(-n // F8_BLOCK), f8_pitch(k)), a_scale.dtype)
+    if out is None:
+        out = _new(stream, (rows, n), out_dtype or torch.bfloat16, a.device)
+    _check_tensor(out, "out", (rows, n), out_dtype or out.dtype)
+    _check(lib().nuna_f8_matmul(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),
+                                None if offsets is None else offsets.data_ptr(), groups, rows, n, k, out.data_ptr(),
+                                kind, _dtype_code(out), _stream(stream)))
+    return out
+
+
+def f8_wgrad(a, a_scale, b, b_scale, offsets, out=None, out_dtype=None, stream=None):
+    """Gradient of grouped weights: out[g] = sum over the rows r of group g of a[:, r] b[:, r]^T.  a [n, width] and
+    b [k, width] with their scales, both of f8_quantize_cols with these offsets.  out [groups, n, k] of out_dtype
+    (float32 unless given), zeros for a group without rows."""
+    torch = _torch()
+    f8 = torch.float8_e4m3fn
+    groups = _check_offsets(offsets)
+    if a.dim() != 2 or b.dim() != 2:
+        raise ValueError("a must be [n, width] and b [k, width]")
+    (n, width), k = a.shape, b.shape[0]
+    rows = width - F8_BLOCK * groups + F8_BLOCK - 1  # the most that this width is the layout of
+    if width % F8_BLOCK or rows < 0:
+        raise ValueError(f"a of {width} columns is no layout of {groups} groups")
+    kind = _scale_kind(a_scale, "a_scale")
+    _check_tensor(a, "a", (n, width), f8)
+    _check_tensor(b, "b", (k, width), f8)
+    _check_tensor(a_scale, "a_scale", (n, f8_pitch(width)), a_scale.dtype)
+    _check_tensor(b_scale, "b_scale", (k, f8_pitch(width)), a_scale.dtype)
+    if out is None:
+        out = _new(stream, (groups, n, k), out_dtype or torch.float32, a.device)
+    _check_tensor(out, "out", (groups, n, k), out_dtype or out.dtype)
+    _check(lib().nuna_f8_wgrad(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), offsets.data_ptr(),
+                               groups, rows, n, k, out.data_ptr(), kind, _dtype_code(out), _stream(stream)))
     return out
 
 
