@@ -30,14 +30,6 @@ namespace {
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
-
-// 32 values of one lane: two vectors of 16 bytes, 64 bytes apart.
-__device__ __forceinline__ i32x8_t load_frag(const uint8_t* p) {
-    const i32x4_t a = *reinterpret_cast<const i32x4_t*>(p);
-    const i32x4_t b = *reinterpret_cast<const i32x4_t*>(p + 64);
-    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 // Eight e4m3 values as bf16, exactly.
@@ -49,132 +41,357 @@ __device__ __forceinline__ bf16x8_t widen_frag(uint32_t a, uint32_t b) {
     return bf16x8_t{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
 }
 
-// The fp32 value of entry i of a scale array.
-template <int KIND>
-__device__ __forceinline__ float scale_value(const void* s, int64_t i) {
-    if constexpr (KIND == kScaleF32) return static_cast<const float*>(s)[i];
-    const uint32_t e = static_cast<const uint8_t*>(s)[i];
+// The fp32 value of an e8m0 byte.
+__device__ __forceinline__ float e8m0_value(uint32_t e) {
     return __uint_as_float(e == 0 ? 0x00400000u : e == 255 ? 0x7fc00000u : e << 23);
+}
+
+// A block's 32 values of one lane: as they are, or widened.
+template <bool PRECISE>
+struct Frag {
+    i32x8_t v;
+};
+template <>
+struct Frag<true> {
+    bf16x8_t v[4];
+};
+
+template <bool PRECISE>
+__device__ __forceinline__ Frag<PRECISE> make_frag(const i32x4_t& a, const i32x4_t& b) {
+    if constexpr (PRECISE)
+        return {{widen_frag(a[0], a[1]), widen_frag(a[2], a[3]), widen_frag(b[0], b[1]), widen_frag(b[2], b[3])}};
+    else
+        return {__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
 }
 
 // The sum of one block of 128 of 16 x 16 outputs, before its scales.
 template <bool PRECISE>
-__device__ __forceinline__ f32x4_t block_sum(const i32x8_t& x, const i32x8_t& y) {
+__device__ __forceinline__ f32x4_t block_sum(const Frag<PRECISE>& x, const Frag<PRECISE>& y) {
     f32x4_t p = {};
     if constexpr (PRECISE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen_frag(x[2 * i], x[2 * i + 1]), widen_frag(y[2 * i], y[2 * i + 1]),
-                                                        p, 0, 0, 0);
+        for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v[i], y.v[i], p, 0, 0, 0);
     } else {
-        p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, p, 0, 0, 0, 0, 0, 0);
+        p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x.v, y.v, p, 0, 0, 0, 0, 0, 0);
     }
     return p;
 }
 
 struct Operand {
     const uint8_t* values;
-    const void* scales;
-    int64_t row_bytes;  // of values
-    int64_t pitch;      // of scales
+    const uint8_t* scales;
+    int64_t row_bytes;    // of values
+    int64_t scale_bytes;  // of a row of scales
 };
 
-template <int OUT>
-__device__ __forceinline__ void store_out(void* out, int64_t at, float v) {
-    Arith<OUT>::store1(out, at, v);
+// ---------------------------------------------------------------- tiles
+
+// Inclusive prefix sum of v over the wave.
+__device__ __forceinline__ int wave_inclusive(int v) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
 }
 
-constexpr int kTile = 64;  // y and x of a workgroup: 4 waves of 32 x 32
+// y tiles of group i, of BY rows each (0 past the last group).
+template <int BY>
+__device__ __forceinline__ int group_tiles(const int32_t* __restrict__ offsets, int i, int groups, int64_t rows) {
+    if (i >= groups) return 0;
+    const int64_t from = group_offset(offsets, i, rows), to = group_offset(offsets, i + 1, rows);
+    return to > from ? static_cast<int>((to - from + BY - 1) / BY) : 0;
+}
 
-// The simple form: fragments straight from memory.
-template <int KIND, bool WGRAD, int OUT>
-__global__ __launch_bounds__(kWG) void k_f8_matmul(Operand Y, Operand X, const int32_t* __restrict__ offsets, int groups,
-                                                   int64_t rows, int64_t ny, int64_t nx, int64_t blocks, int64_t ytiles,
-                                                   int64_t xtiles, int64_t items, void* __restrict__ out) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int l16 = lane & 15, quad = lane >> 4;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int64_t xt = item % xtiles;
-        int64_t yt = item / xtiles;
-        int64_t yfrom = 0, yto = ny, kb0 = 0, kb1 = blocks, g = 0;
-        if constexpr (WGRAD) {
-            g = yt / ytiles;
-            yt -= g * ytiles;
-            const int64_t from = group_offset(offsets, g, rows), to = group_offset(offsets, g + 1, rows);
-            kb0 = from / kF8Block + g;
-            kb1 = kb0 + (to > from ? (to - from + kF8Block - 1) / kF8Block : 0);
-        } else if (offsets) {
-            for (; g < groups; ++g) {
-                yfrom = group_offset(offsets, g, rows);
-                yto = group_offset(offsets, g + 1, rows);
-                const int64_t tiles = yto > yfrom ? (yto - yfrom + kTile - 1) / kTile : 0;
-                if (yt < tiles) break;
-                yt -= tiles;
-            }
-            if (g == groups) continue;
+struct Tile {
+    int g;         // group
+    int y0, yend;  // first row, and end of the group's rows
+    int xt;        // x tile
+    int kb0, kb1;  // blocks to sum
+};
+
+struct Shape {
+    const int32_t* offsets;
+    int groups;
+    int rows;    // that the offsets are cut to
+    int ny, nx;  // of a product: rows (all groups') and columns
+    int blocks;  // summed by nuna_f8_matmul
+    int xtiles;
+    int items;   // workgroups that the tiles need at most
+};
+
+constexpr int kBand = 8;  // y tiles that are walked together along x
+
+// In a group of ytiles x xtiles tiles, tile t: bands of kBand y tiles, along x, so that the tiles that run together
+// share both their operands.
+__device__ __forceinline__ void band_order(uint32_t t, uint32_t ytiles, uint32_t xtiles, int& yt, int& xt) {
+    const uint32_t band = t / (kBand * xtiles);
+    const uint32_t h = min(static_cast<uint32_t>(kBand), ytiles - band * kBand);
+    const uint32_t in = t - band * kBand * xtiles;
+    xt = static_cast<int>(in / h);
+    yt = static_cast<int>(band * kBand + in - xt * h);
+}
+
+// The tile of work item `item`, or false.  Workgroup b runs on XCD b mod 8: each XCD takes a run of consecutive
+// tiles, so that a group's weights are read into one L2.
+template <int BY, bool WGRAD>
+__device__ __forceinline__ bool find_tile(const Shape& s, uint32_t item, Tile& tile) {
+    const uint32_t xcd = item & 7, seq = item >> 3;
+    const auto of_all = [&](uint32_t all, uint32_t& t) {
+        const uint32_t per = (all + 7) / 8;
+        t = xcd * per + seq;
+        return seq < per && t < all;
+    };
+    uint32_t t;
+    int yt;
+    if constexpr (WGRAD) {
+        const uint32_t ytiles = (s.ny + BY - 1) / BY, each = ytiles * s.xtiles;
+        if (!of_all(each * s.groups, t)) return false;
+        tile.g = static_cast<int>(t / each);
+        band_order(t - tile.g * each, ytiles, s.xtiles, yt, tile.xt);
+        const int from = group_offset(s.offsets, tile.g, s.rows), to = group_offset(s.offsets, tile.g + 1, s.rows);
+        tile.y0 = yt * BY;
+        tile.yend = s.ny;
+        tile.kb0 = from / kF8Block + tile.g;
+        tile.kb1 = tile.kb0 + (to > from ? (to - from + kF8Block - 1) / kF8Block : 0);
+        return true;
+    } else {
+        tile.kb0 = 0;
+        tile.kb1 = s.blocks;
+        if (!s.offsets) {
+            const uint32_t ytiles = (s.ny + BY - 1) / BY;
+            if (!of_all(ytiles * s.xtiles, t)) return false;
+            band_order(t, ytiles, s.xtiles, yt, tile.xt);
+            tile.g = 0;
+            tile.y0 = yt * BY;
+            tile.yend = s.ny;
+            return true;
         }
-        const int64_t y0 = yfrom + yt * kTile + (wave >> 1) * 32, x0 = xt * kTile + (wave & 1) * 32;
-        if (y0 >= yto || x0 >= nx) continue;
-        const int64_t xbase = WGRAD ? 0 : g * nx;                                       // rows of X before this group's
-        const int64_t xsbase = WGRAD ? 0 : g * ((nx + kF8Block - 1) / kF8Block);          // rows of its scales
-        constexpr bool kPrecise = OUT == kDtF32;
-        constexpr bool kScaledOp = KIND == kScaleE8m0 && !kPrecise;  // the scales are operands
-        f32x4_t acc[2][2] = {};
-        for (int64_t kb = kb0; kb < kb1; ++kb) {
-            i32x8_t fy[2], fx[2];
-            float sy[2];
-            int ey[2];
-            for (int i = 0; i < 2; ++i) {
-                const int64_t y = std::min(y0 + 16 * i + l16, yto - 1), x = std::min(x0 + 16 * i + l16, nx - 1);
-                fy[i] = load_frag(Y.values + y * Y.row_bytes + kb * kF8Block + quad * 16);
-                fx[i] = load_frag(X.values + (xbase + x) * X.row_bytes + kb * kF8Block + quad * 16);
-                if constexpr (!kScaledOp)
-                    sy[i] = scale_value<KIND>(Y.scales, y * Y.pitch + kb);
-                else
-                    ey[i] = static_cast<const uint8_t*>(Y.scales)[y * Y.pitch + kb];
+        const int lane = threadIdx.x & 63;
+        uint32_t total = 0;
+        for (int i = 0; i < s.groups; i += 64)
+            total += __builtin_amdgcn_readlane(wave_inclusive(group_tiles<BY>(s.offsets, i + lane, s.groups, s.rows)), 63);
+        if (!of_all(total * s.xtiles, t)) return false;
+        uint32_t before = 0;
+        for (int i = 0; i < s.groups; i += 64) {
+            const int n = group_tiles<BY>(s.offsets, i + lane, s.groups, s.rows);
+            const int upto = wave_inclusive(n);
+            const uint64_t past = __ballot((before + upto) * s.xtiles > t);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                const uint32_t ytiles = __builtin_amdgcn_readlane(n, l);
+                const uint32_t first = before + __builtin_amdgcn_readlane(upto, l) - ytiles;
+                band_order(t - first * s.xtiles, ytiles, s.xtiles, yt, tile.xt);
+                tile.g = __builtin_amdgcn_readfirstlane(i + l);
+                tile.y0 = static_cast<int>(group_offset(s.offsets, i + l, s.rows)) + yt * BY;
+                tile.yend = static_cast<int>(group_offset(s.offsets, i + l + 1, s.rows));
+                return true;
             }
-            for (int j = 0; j < 2; ++j) {
-                if constexpr (kScaledOp) {
-                    const int64_t x = std::min(x0 + 16 * j + l16, nx - 1);
-                    const int64_t srow = WGRAD ? x : xsbase + x / kF8Block;
-                    const int ex = static_cast<const uint8_t*>(X.scales)[srow * X.pitch + kb];
-                    for (int i = 0; i < 2; ++i)
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx[j], fy[i], acc[i][j], 0, 0, 0, ex, 0,
-                                                                                     ey[i]);
-                } else {
-                    float sx[4];
-                    for (int r = 0; r < 4; ++r) {
-                        const int64_t x = std::min(x0 + 16 * j + quad * 4 + r, nx - 1);
-                        const int64_t srow = WGRAD ? x : xsbase + x / kF8Block;
-                        sx[r] = scale_value<KIND>(X.scales, srow * X.pitch + kb);
-                    }
-                    for (int i = 0; i < 2; ++i) {
-                        const f32x4_t p = block_sum<kPrecise>(fx[j], fy[i]);
-                        for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(p[r], sy[i] * sx[r], acc[i][j][r]);
-                    }
-                }
-            }
+            before += __builtin_amdgcn_readlane(upto, 63);
         }
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < 2; ++j)
-                for (int r = 0; r < 4; ++r) {
-                    const int64_t y = y0 + 16 * i + l16, x = x0 + 16 * j + quad * 4 + r;
-                    if (y < yto && x < nx) store_out<OUT>(out, ((WGRAD ? g * ny : 0) + y) * nx + x, acc[i][j][r]);
-                }
+        return false;
     }
 }
 
-template <bool WGRAD>
-hipError_t launch(const Operand& Y, const Operand& X, const int32_t* offsets, int groups, int64_t rows, int64_t ny,
-                  int64_t nx, int64_t blocks, void* out, int kind, int out_dtype, hipStream_t stream) {
+typedef const __attribute__((address_space(1))) void* global_ptr_t;
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef const __attribute__((address_space(4))) uint32_t* scalar_ptr_t;  // read by scalar loads
+
+// 16 bytes a lane from memory to LDS at `to` + 16 lane, without registers between.
+__device__ __forceinline__ void copy_to_lds16(const uint8_t* from, uint8_t* to) {
+    __builtin_amdgcn_global_load_lds((global_ptr_t)from, (lds_ptr_t)to, 16, 0, 0);
+}
+__device__ __forceinline__ void copy_to_lds4(const uint8_t* from, uint8_t* to) {
+    __builtin_amdgcn_global_load_lds((global_ptr_t)from, (lds_ptr_t)to, 4, 0, 0);
+}
+
+// Both operands through LDS: tiles of BY x BX outputs, waves WY x WX, one block of 128 a step.  While a step is
+// computed the next one's operands are copied to the other half of LDS.  A row's eight 16-byte parts are kept in the
+// order part ^ (row % 8), so that the 16 rows that a fragment reads lie in different banks.
+template <int BY, int BX, int WY, int WX, int KIND, bool WGRAD, int OUT>
+__global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X, Shape shape, void* __restrict__ out) {
+    constexpr int NW = WY * WX, TY = BY / WY / 16, TX = BX / WX / 16;  // waves; 16 x 16 tiles of a wave
+    constexpr bool kPrecise = OUT == kDtF32;
+    constexpr bool kScaledOp = KIND == kScaleE8m0 && !kPrecise;  // the scales are operands
+    constexpr int kStage = (BY + BX) * kF8Block;
+    constexpr int kCopies = (BY + BX) / 8 / NW;  // of 8 rows, a wave
+    constexpr int kSS = KIND == kScaleF32 ? 4 : 1;
+    constexpr int kScaleRows = BY + (WGRAD ? BX : 0);
+    constexpr int kScaleStage = kScaleRows * 4 * kSS;  // four blocks' scales of each row
+    static_assert(kCopies * NW * 8 == BY + BX && BX / WX <= kF8Block, "whole copies, and one x scale a wave");
+    __shared__ __align__(1024) uint8_t lds[2 * kStage + 2 * kScaleStage];
+    uint8_t* const lds_scale = lds + 2 * kStage;
+
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wy = wave / WX, wx = wave % WX;
+    // This lane's part of a fragment: 16 bytes at `part0`, and 16 more whose part is 4 on.
+    const int part0 = l16 * kF8Block + ((quad ^ (l16 & 7)) * 16), part1 = part0 ^ 64;
+    for (int item = blockIdx.x; item < shape.items; item += gridDim.x) {
+        Tile t;
+        if (!find_tile<BY, WGRAD>(shape, item, t)) continue;
+        const int x0 = t.xt * BX;
+        const int64_t xrow0 = WGRAD ? 0 : static_cast<int64_t>(t.g) * shape.nx;
+        const int xblocks = (shape.nx + kF8Block - 1) / kF8Block;
+
+        // What this lane copies: rows past the end are the last row again, whose outputs are not stored.
+        const uint8_t* from[kCopies];
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int r = (wave * kCopies + i) * 8 + (lane >> 3);
+            const int part = (lane & 7) ^ (lane >> 3);
+            if (wave * kCopies + i < BY / 8)
+                from[i] = Y.values + min(t.y0 + r, t.yend - 1) * Y.row_bytes + part * 16 + int64_t(t.kb0) * kF8Block;
+            else
+                from[i] = X.values + (xrow0 + min(x0 + r - BY, shape.nx - 1)) * X.row_bytes + part * 16 + int64_t(t.kb0) * kF8Block;
+        }
+        const auto copy_next = [&](int half) {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                copy_to_lds16(from[i], lds + half * kStage + (wave * kCopies + i) * 1024);
+                from[i] += kF8Block;
+            }
+        };
+        const auto copy_scales = [&](int quartet, int half) {
+            for (int i = wave; i < kScaleRows / 64; i += NW) {
+                const int r = i * 64 + lane;
+                const uint8_t* p = r < BY ? Y.scales + min(t.y0 + r, t.yend - 1) * Y.scale_bytes
+                                          : X.scales + min(x0 + r - BY, shape.nx - 1) * X.scale_bytes;
+                if constexpr (kSS == 4)
+                    copy_to_lds16(p + quartet * 16, lds_scale + half * kScaleStage + i * 1024);
+                else
+                    copy_to_lds4(p + quartet * 4, lds_scale + half * kScaleStage + i * 256);
+            }
+        };
+        // The scales that all of a wave's x share: the word that holds block kb's (e8m0: four blocks').
+        const int64_t xs_row = WGRAD ? 0 : static_cast<int64_t>(t.g) * xblocks + min((x0 + wx * TX * 16) / kF8Block, xblocks - 1);
+        const scalar_ptr_t xs = (scalar_ptr_t)(X.scales + xs_row * X.scale_bytes);
+        const auto x_scale_word = [&](int kb) { return xs[KIND == kScaleF32 ? kb : kb >> 2]; };
+
+        f32x4_t acc[TY][TX];
+#pragma unroll
+        for (int i = 0; i < TY; ++i)
+#pragma unroll
+            for (int j = 0; j < TX; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        const bool busy = t.y0 + wy * TY * 16 < t.yend && x0 + wx * TX * 16 < shape.nx;
+
+        uint32_t xs_next = 0;
+        if (t.kb0 < t.kb1) {
+            copy_next(0);
+            copy_scales(t.kb0 >> 2, (t.kb0 >> 2) & 1);
+            if constexpr (!WGRAD) xs_next = x_scale_word(t.kb0);
+        }
+        for (int kb = t.kb0; kb < t.kb1; ++kb) {
+            const int half = (kb - t.kb0) & 1;
+            const uint32_t xs_now = xs_next;
+            __syncthreads();  // this step's operands are there, and the last step's have been read
+            if (kb + 1 < t.kb1) {
+                copy_next(half ^ 1);
+                if (((kb + 1) & 3) == 0) copy_scales((kb + 1) >> 2, ((kb + 1) >> 2) & 1);
+                if constexpr (!WGRAD) xs_next = x_scale_word(kb + 1);
+            }
+            if (!busy) continue;
+            const uint8_t* const ly = lds + half * kStage + wy * TY * 16 * kF8Block;
+            const uint8_t* const lx = lds + half * kStage + (BY + wx * TX * 16) * kF8Block;
+            const uint8_t* const ls = lds_scale + ((kb >> 2) & 1) * kScaleStage + (kb & 3) * kSS;
+            const auto frag = [&](const uint8_t* base, int tile16) {
+                return make_frag<kPrecise>(*reinterpret_cast<const i32x4_t*>(base + part0 + tile16 * 16 * kF8Block),
+                                           *reinterpret_cast<const i32x4_t*>(base + part1 + tile16 * 16 * kF8Block));
+            };
+            Frag<kPrecise> fy[TY];
+            float sy[TY];
+            int ey[TY];
+#pragma unroll
+            for (int i = 0; i < TY; ++i) {
+                fy[i] = frag(ly, i);
+                const uint8_t* p = ls + ((wy * TY + i) * 16 + l16) * 4 * kSS;
+                if constexpr (KIND == kScaleF32)
+                    sy[i] = *reinterpret_cast<const float*>(p);
+                else if constexpr (kScaledOp)
+                    ey[i] = *p;
+                else
+                    sy[i] = e8m0_value(*p);
+            }
+            const int ex_all = static_cast<int>(xs_now >> (8 * (kb & 3)) & 255u);
+            if constexpr (!WGRAD && !kScaledOp) {
+                const float sx = KIND == kScaleF32 ? __uint_as_float(xs_now) : e8m0_value(ex_all);
+#pragma unroll
+                for (int i = 0; i < TY; ++i) sy[i] *= sx;
+            }
+#pragma unroll
+            for (int j = 0; j < TX; ++j) {
+                const Frag<kPrecise> fx = frag(lx, j);
+                if constexpr (kScaledOp) {
+                    int ex = ex_all;
+                    if constexpr (WGRAD) ex = ls[(BY + (wx * TX + j) * 16 + l16) * 4];
+#pragma unroll
+                    for (int i = 0; i < TY; ++i)
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx.v, fy[i].v, acc[i][j], 0, 0, 0, ex, 0,
+                                                                                     ey[i]);
+                } else {
+                    float sx[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+                    if constexpr (WGRAD) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const uint8_t* p = ls + (BY + (wx * TX + j) * 16 + quad * 4 + r) * 4 * kSS;
+                            sx[r] = KIND == kScaleF32 ? *reinterpret_cast<const float*>(p) : e8m0_value(*p);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < TY; ++i) {
+                        const f32x4_t p = block_sum<kPrecise>(fx, fy[i]);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            acc[i][j][r] = fmaf(p[r], WGRAD ? sy[i] * sx[r] : sy[i], acc[i][j][r]);
+                    }
+                }
+            }
+        }
+        __syncthreads();  // the last step's operands have been read
+        // Four outputs of a lane lie together.
+        constexpr int ES = Arith<OUT>::kEsize;
+        const bool whole = (shape.nx & 3) == 0;
+#pragma unroll
+        for (int i = 0; i < TY; ++i) {
+            const int y = t.y0 + (wy * TY + i) * 16 + l16;
+            if (y >= t.yend) continue;
+            char* const row = static_cast<char*>(out) + ((WGRAD ? static_cast<int64_t>(t.g) * shape.ny : 0) + y) * shape.nx * ES;
+#pragma unroll
+            for (int j = 0; j < TX; ++j) {
+                const int x = x0 + (wx * TX + j) * 16 + quad * 4;
+                if (x + 4 <= shape.nx && whole) {
+                    if constexpr (OUT == kDtF32)
+                        *reinterpret_cast<f32x4_t*>(row + x * ES) = acc[i][j];
+                    else
+                        *reinterpret_cast<uint2*>(row + x * ES) =
+                            make_uint2(f32_to_bf16x2(acc[i][j][0], acc[i][j][1]), f32_to_bf16x2(acc[i][j][2], acc[i][j][3]));
+                } else {
+                    for (int r = 0; r < 4; ++r)
+                        if (x + r < shape.nx) Arith<OUT>::store1(row, x + r, acc[i][j][r]);
+                }
+            }
+        }
+    }
+}
+
+template <int BY, int BX, int WY, int WX, bool WGRAD>
+hipError_t launch_tiles(const Operand& Y, const Operand& X, Shape shape, void* out, int kind, int out_dtype,
+                        hipStream_t stream) {
+    const int64_t xtiles = (static_cast<int64_t>(shape.nx) + BX - 1) / BX;
     // A group's last tile may be part full: at most one more tile a group that has a row.
-    int64_t ytiles = (ny + kTile - 1) / kTile;
-    int64_t all = WGRAD ? ytiles * groups : offsets ? ny / kTile + std::min<int64_t>(groups, ny) : ytiles;
-    const int64_t xtiles = (nx + kTile - 1) / kTile, items = all * xtiles;
+    const int64_t ytiles = WGRAD ? (static_cast<int64_t>(shape.ny) + BY - 1) / BY * shape.groups
+                                 : shape.offsets ? shape.ny / BY + std::min(shape.groups, shape.ny)
+                                                 : (shape.ny + BY - 1) / BY;
+    const int64_t items = (ytiles * xtiles + 7) / 8 * 8;
+    if (items > INT32_MAX - (1 << 20)) return hipErrorInvalidValue;  // more outputs than the memory holds
+    shape.xtiles = static_cast<int>(xtiles);
+    shape.items = static_cast<int>(items);
     const int64_t grid = std::min(items, grid_limit(int64_t(1) << 20));
     const auto go = [&](auto kd, auto od) {
-        k_f8_matmul<decltype(kd)::value, WGRAD, decltype(od)::value><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(
-            Y, X, offsets, groups, rows, ny, nx, blocks, ytiles, xtiles, items, out);
+        k_f8_tiles<BY, BX, WY, WX, decltype(kd)::value, WGRAD, decltype(od)::value>
+            <<<static_cast<uint32_t>(grid), WY * WX * 64, 0, stream>>>(Y, X, shape, out);
     };
     const auto typed = [&](auto kd) {
         if (out_dtype == kDtBf16)
@@ -186,7 +403,7 @@ hipError_t launch(const Operand& Y, const Operand& X, const int32_t* offsets, in
         typed(std::integral_constant<int, kScaleF32>{});
     else
         typed(std::integral_constant<int, kScaleE8m0>{});
-    note_launch(WGRAD ? "k_f8_wgrad" : "k_f8_matmul", kMapLinear, 1, grid, kWG, 1);
+    note_launch(WGRAD ? "k_f8_tiles_wgrad" : "k_f8_tiles", kMapLinear, 1, grid, WY * WX * 64, 1);
     return hipGetLastError();
 }
 
@@ -195,18 +412,24 @@ hipError_t launch(const Operand& Y, const Operand& X, const int32_t* offsets, in
 hipError_t launch_f8_matmul(const void* a, const void* a_scale, const void* b, const void* b_scale,
                             const int32_t* offsets, int groups, int64_t rows, int64_t n, int64_t k, void* out, int kind,
                             int out_dtype, hipStream_t stream) {
-    const Operand Y = {static_cast<const uint8_t*>(a), a_scale, k, f8_pitch(k)};
-    const Operand X = {static_cast<const uint8_t*>(b), b_scale, k, f8_pitch(k)};
-    return launch<false>(Y, X, offsets, groups, rows, rows, n, k / kF8Block, out, kind, out_dtype, stream);
+    const int64_t scale_bytes = f8_pitch(k) * static_cast<int64_t>(f8_scale_size(kind));
+    const Operand Y = {static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(a_scale), k, scale_bytes};
+    const Operand X = {static_cast<const uint8_t*>(b), static_cast<const uint8_t*>(b_scale), k, scale_bytes};
+    const Shape shape = {offsets, groups, static_cast<int>(rows), static_cast<int>(rows), static_cast<int>(n),
+                         static_cast<int>(k / kF8Block), 0, 0};
+    if (rows / groups > 128) return launch_tiles<256, 256, 4, 2, false>(Y, X, shape, out, kind, out_dtype, stream);
+    return launch_tiles<64, 128, 2, 2, false>(Y, X, shape, out, kind, out_dtype, stream);
 }
 
 hipError_t launch_f8_wgrad(const void* a, const void* a_scale, const void* b, const void* b_scale,
                            const int32_t* offsets, int groups, int64_t rows, int64_t n, int64_t k, void* out, int kind,
                            int out_dtype, hipStream_t stream) {
     const int64_t width = f8_t_width(rows, groups);
-    const Operand Y = {static_cast<const uint8_t*>(a), a_scale, width, f8_pitch(width)};
-    const Operand X = {static_cast<const uint8_t*>(b), b_scale, width, f8_pitch(width)};
-    return launch<true>(Y, X, offsets, groups, rows, n, k, 0, out, kind, out_dtype, stream);
+    const int64_t scale_bytes = f8_pitch(width) * static_cast<int64_t>(f8_scale_size(kind));
+    const Operand Y = {static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(a_scale), width, scale_bytes};
+    const Operand X = {static_cast<const uint8_t*>(b), static_cast<const uint8_t*>(b_scale), width, scale_bytes};
+    const Shape shape = {offsets, groups, static_cast<int>(rows), static_cast<int>(n), static_cast<int>(k), 0, 0, 0};
+    return launch_tiles<128, 128, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
 }
 
 }  // namespace nuna
