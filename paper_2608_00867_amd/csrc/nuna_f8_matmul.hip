@@ -320,31 +320,53 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
 #pragma unroll
                 for (int i = 0; i < TY; ++i) sy[i] *= sx;
             }
+            if constexpr (kScaledOp) {
+                Frag<kPrecise> fx[2];
+                fx[0] = frag(lx, 0);
 #pragma unroll
-            for (int j = 0; j < TX; ++j) {
-                const Frag<kPrecise> fx = frag(lx, j);
-                if constexpr (kScaledOp) {
+                for (int j = 0; j < TX; ++j) {
+                    if (j + 1 < TX) fx[(j + 1) & 1] = frag(lx, j + 1);
+                    __builtin_amdgcn_sched_barrier(0);
                     int ex = ex_all;
                     if constexpr (WGRAD) ex = ls[(BY + (wx * TX + j) * 16 + l16) * 4];
 #pragma unroll
                     for (int i = 0; i < TY; ++i)
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx.v, fy[i].v, acc[i][j], 0, 0, 0, ex, 0,
-                                                                                     ey[i]);
-                } else {
-                    float sx[4] = {1.0f, 1.0f, 1.0f, 1.0f};
-                    if constexpr (WGRAD) {
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx[j & 1].v, fy[i].v, acc[i][j], 0, 0, 0,
+                                                                                     ex, 0, ey[i]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                // The products of column j run in the matrix unit while those of j - 1 are scaled and added.  The
+                // fences keep that order: left alone, the compiler waits for each product to add it at once.
+                f32x4_t p[2][TY];
+                float sx[2][4];
+                Frag<kPrecise> fx[2];
+                fx[0] = frag(lx, 0);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const uint8_t* p = ls + (BY + (wx * TX + j) * 16 + quad * 4 + r) * 4 * kSS;
-                            sx[r] = KIND == kScaleF32 ? *reinterpret_cast<const float*>(p) : e8m0_value(*p);
+                for (int j = 0; j <= TX; ++j) {
+                    if (j + 1 < TX) fx[(j + 1) & 1] = frag(lx, j + 1);
+                    if constexpr (WGRAD) {
+                        if (j < TX) {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const uint8_t* q = ls + (BY + (wx * TX + j) * 16 + quad * 4 + r) * 4 * kSS;
+                                sx[j & 1][r] = KIND == kScaleF32 ? *reinterpret_cast<const float*>(q) : e8m0_value(*q);
+                            }
                         }
                     }
 #pragma unroll
                     for (int i = 0; i < TY; ++i) {
-                        const f32x4_t p = block_sum<kPrecise>(fx, fy[i]);
+                        if (j < TX) {
+                            if constexpr (!kPrecise) __builtin_amdgcn_sched_barrier(0);
+                            p[j & 1][i] = block_sum<kPrecise>(fx[j & 1], fy[i]);
+                            if constexpr (!kPrecise) __builtin_amdgcn_sched_barrier(0);
+                        }
+                        if (j > 0) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            acc[i][j][r] = fmaf(p[r], WGRAD ? sy[i] * sx[r] : sy[i], acc[i][j][r]);
+                            for (int r = 0; r < 4; ++r)
+                                acc[i][j - 1][r] = fmaf(p[(j - 1) & 1][i][r], WGRAD ? sy[i] * sx[(j - 1) & 1][r] : sy[i],
+                                                        acc[i][j - 1][r]);
+                        }
                     }
                 }
             }
