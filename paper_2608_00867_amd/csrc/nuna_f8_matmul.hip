@@ -195,16 +195,25 @@ __device__ __forceinline__ bool find_tile(const Shape& s, uint32_t item, Tile& t
     }
 }
 
-typedef const __attribute__((address_space(1))) void* global_ptr_t;
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
-typedef const __attribute__((address_space(4))) uint32_t* scalar_ptr_t;  // read by scalar loads
+typedef __amdgpu_buffer_rsrc_t buffer_t;
 
-// 16 bytes a lane from memory to LDS at `to` + 16 lane, without registers between.
-__device__ __forceinline__ void copy_to_lds16(const uint8_t* from, uint8_t* to) {
-    __builtin_amdgcn_global_load_lds((global_ptr_t)from, (lds_ptr_t)to, 16, 0, 0);
+// The memory from `p` on as a buffer, which the copies to LDS read at a 32-bit offset a lane and one for the wave.
+// (The copies that take addresses are flat instructions to the compiler: while one is under way it waits for all
+// LDS reads wherever it would wait for one, which took a fifth of the time.)
+__device__ __forceinline__ buffer_t make_buffer(const uint8_t* p) {
+    const uint64_t v = reinterpret_cast<uint64_t>(p);  // the same in all lanes
+    const uint64_t u = static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32))) << 32 |
+                       static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(u), 0, 0xffffffff, 0x00027000);
 }
-__device__ __forceinline__ void copy_to_lds4(const uint8_t* from, uint8_t* to) {
-    __builtin_amdgcn_global_load_lds((global_ptr_t)from, (lds_ptr_t)to, 4, 0, 0);
+
+// 16 (or 4) bytes a lane from memory to LDS at `to` + 16 (4) times the lane, without registers between.
+__device__ __forceinline__ void copy_to_lds16(buffer_t from, uint32_t lane_offset, uint32_t offset, uint8_t* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_ptr_t)to, 16, lane_offset, offset, 0, 0);
+}
+__device__ __forceinline__ void copy_to_lds4(buffer_t from, uint32_t lane_offset, uint32_t offset, uint8_t* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_ptr_t)to, 4, lane_offset, offset, 0, 0);
 }
 
 // Both operands through LDS: tiles of BY x BX outputs, waves WY x WX, one block of 128 a step.  While a step is
@@ -218,9 +227,9 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
     constexpr int kStage = (BY + BX) * kF8Block;
     constexpr int kCopies = (BY + BX) / 8 / NW;  // of 8 rows, a wave
     constexpr int kSS = KIND == kScaleF32 ? 4 : 1;
-    constexpr int kScaleRows = BY + (WGRAD ? BX : 0);
-    constexpr int kScaleStage = kScaleRows * 4 * kSS;  // four blocks' scales of each row
-    static_assert(kCopies * NW * 8 == BY + BX && BX / WX <= kF8Block, "whole copies, and one x scale a wave");
+    constexpr int kScaleRows = BY + (WGRAD ? BX : (BX + kF8Block - 1) / kF8Block);
+    constexpr int kScaleStage = (kScaleRows + 3) / 4 * 16 * kSS;  // four blocks' scales of each row
+    static_assert(kCopies * NW * 8 == BY + BX && BX / WX <= kF8Block && BY % 64 == 0, "whole copies, and one x scale a wave");
     __shared__ __align__(1024) uint8_t lds[2 * kStage + 2 * kScaleStage];
     uint8_t* const lds_scale = lds + 2 * kStage;
 
@@ -236,39 +245,49 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
         const int64_t xrow0 = WGRAD ? 0 : static_cast<int64_t>(t.g) * shape.nx;
         const int xblocks = (shape.nx + kF8Block - 1) / kF8Block;
 
-        // What this lane copies: rows past the end are the last row again, whose outputs are not stored.
-        const uint8_t* from[kCopies];
+        // What this lane copies, from the tile's first rows on: rows past the end are the last row again, whose
+        // outputs are not stored.
+        const int ylast = t.yend - 1 - t.y0, xlast = shape.nx - 1 - x0;
+        const buffer_t ybuf = make_buffer(Y.values + t.y0 * Y.row_bytes);
+        const buffer_t xbuf = make_buffer(X.values + (xrow0 + x0) * X.row_bytes);
+        uint32_t from[kCopies];
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
             const int r = (wave * kCopies + i) * 8 + (lane >> 3);
-            const int part = (lane & 7) ^ (lane >> 3);
+            const uint32_t part = ((lane & 7) ^ (lane >> 3)) * 16;
             if (wave * kCopies + i < BY / 8)
-                from[i] = Y.values + min(t.y0 + r, t.yend - 1) * Y.row_bytes + part * 16 + int64_t(t.kb0) * kF8Block;
+                from[i] = min(r, ylast) * static_cast<uint32_t>(Y.row_bytes) + part;
             else
-                from[i] = X.values + (xrow0 + min(x0 + r - BY, shape.nx - 1)) * X.row_bytes + part * 16 + int64_t(t.kb0) * kF8Block;
+                from[i] = min(r - BY, xlast) * static_cast<uint32_t>(X.row_bytes) + part;
         }
-        const auto copy_next = [&](int half) {
+        const auto copy = [&](int kb, int half) {
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) {
-                copy_to_lds16(from[i], lds + half * kStage + (wave * kCopies + i) * 1024);
-                from[i] += kF8Block;
-            }
+            for (int i = 0; i < kCopies; ++i)
+                copy_to_lds16(wave * kCopies + i < BY / 8 ? ybuf : xbuf, from[i], kb * kF8Block,
+                              lds + half * kStage + (wave * kCopies + i) * 1024);
         };
+        const buffer_t ysbuf = make_buffer(Y.scales + t.y0 * Y.scale_bytes);
+        const int xsrow0 = WGRAD ? x0 : x0 / kF8Block, xslast = (WGRAD ? shape.nx : xblocks) - 1 - xsrow0;
+        const buffer_t xsbuf = make_buffer(X.scales + ((WGRAD ? 0 : static_cast<int64_t>(t.g) * xblocks) + xsrow0) * X.scale_bytes);
         const auto copy_scales = [&](int quartet, int half) {
-            for (int i = wave; i < kScaleRows / 64; i += NW) {
-                const int r = i * 64 + lane;
-                const uint8_t* p = r < BY ? Y.scales + min(t.y0 + r, t.yend - 1) * Y.scale_bytes
-                                          : X.scales + min(x0 + r - BY, shape.nx - 1) * X.scale_bytes;
+            uint8_t* const to = lds_scale + half * kScaleStage;
+            const auto copy_rows = [&](buffer_t buf, int64_t row_bytes, int r, int last, uint8_t* at) {
+                const uint32_t offset = min(r, last) * static_cast<uint32_t>(row_bytes);
                 if constexpr (kSS == 4)
-                    copy_to_lds16(p + quartet * 16, lds_scale + half * kScaleStage + i * 1024);
+                    copy_to_lds16(buf, offset, quartet * 16, at);
                 else
-                    copy_to_lds4(p + quartet * 4, lds_scale + half * kScaleStage + i * 256);
+                    copy_to_lds4(buf, offset, quartet * 4, at);
+            };
+            for (int i = wave; i < BY / 64; i += NW)
+                copy_rows(ysbuf, Y.scale_bytes, i * 64 + lane, ylast, to + i * 256 * kSS);
+            uint8_t* const xto = to + BY * 4 * kSS;
+            if constexpr (WGRAD) {
+                for (int i = NW - 1 - wave; i < BX / 64; i += NW)
+                    copy_rows(xsbuf, X.scale_bytes, i * 64 + lane, xslast, xto + i * 256 * kSS);
+            } else if (wave == NW - 1 && lane < kScaleRows - BY) {
+                copy_rows(xsbuf, X.scale_bytes, lane, xslast, xto);
             }
         };
-        // The scales that all of a wave's x share: the word that holds block kb's (e8m0: four blocks').
-        const int64_t xs_row = WGRAD ? 0 : static_cast<int64_t>(t.g) * xblocks + min((x0 + wx * TX * 16) / kF8Block, xblocks - 1);
-        const scalar_ptr_t xs = (scalar_ptr_t)(X.scales + xs_row * X.scale_bytes);
-        const auto x_scale_word = [&](int kb) { return xs[KIND == kScaleF32 ? kb : kb >> 2]; };
 
         f32x4_t acc[TY][TX];
 #pragma unroll
@@ -277,20 +296,16 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
             for (int j = 0; j < TX; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         const bool busy = t.y0 + wy * TY * 16 < t.yend && x0 + wx * TX * 16 < shape.nx;
 
-        uint32_t xs_next = 0;
         if (t.kb0 < t.kb1) {
-            copy_next(0);
+            copy(t.kb0, 0);
             copy_scales(t.kb0 >> 2, (t.kb0 >> 2) & 1);
-            if constexpr (!WGRAD) xs_next = x_scale_word(t.kb0);
         }
         for (int kb = t.kb0; kb < t.kb1; ++kb) {
             const int half = (kb - t.kb0) & 1;
-            const uint32_t xs_now = xs_next;
             __syncthreads();  // this step's operands are there, and the last step's have been read
             if (kb + 1 < t.kb1) {
-                copy_next(half ^ 1);
+                copy(kb + 1, half ^ 1);
                 if (((kb + 1) & 3) == 0) copy_scales((kb + 1) >> 2, ((kb + 1) >> 2) & 1);
-                if constexpr (!WGRAD) xs_next = x_scale_word(kb + 1);
             }
             if (!busy) continue;
             const uint8_t* const ly = lds + half * kStage + wy * TY * 16 * kF8Block;
@@ -300,9 +315,11 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
                 return make_frag<kPrecise>(*reinterpret_cast<const i32x4_t*>(base + part0 + tile16 * 16 * kF8Block),
                                            *reinterpret_cast<const i32x4_t*>(base + part1 + tile16 * 16 * kF8Block));
             };
-            Frag<kPrecise> fy[TY];
-            float sy[TY];
-            int ey[TY];
+            // What the first product needs is read first.
+            Frag<kPrecise> fx[2], fy[TY];
+            float sy[TY], sx_all = 0.0f;
+            int ey[TY], ex_all = 0;
+            fx[0] = frag(lx, 0);
 #pragma unroll
             for (int i = 0; i < TY; ++i) {
                 fy[i] = frag(ly, i);
@@ -313,16 +330,22 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
                     ey[i] = *p;
                 else
                     sy[i] = e8m0_value(*p);
+                if (i == 0 && !WGRAD) {
+                    const uint8_t* q = ls + (BY + wx * TX * 16 / kF8Block) * 4 * kSS;
+                    if constexpr (KIND == kScaleF32)
+                        sx_all = *reinterpret_cast<const float*>(q);
+                    else if constexpr (kScaledOp)
+                        ex_all = *q;
+                    else
+                        sx_all = e8m0_value(*q);
+                }
+                if constexpr (!kPrecise) __builtin_amdgcn_sched_barrier(0);
             }
-            const int ex_all = static_cast<int>(xs_now >> (8 * (kb & 3)) & 255u);
             if constexpr (!WGRAD && !kScaledOp) {
-                const float sx = KIND == kScaleF32 ? __uint_as_float(xs_now) : e8m0_value(ex_all);
 #pragma unroll
-                for (int i = 0; i < TY; ++i) sy[i] *= sx;
+                for (int i = 0; i < TY; ++i) sy[i] *= sx_all;
             }
             if constexpr (kScaledOp) {
-                Frag<kPrecise> fx[2];
-                fx[0] = frag(lx, 0);
 #pragma unroll
                 for (int j = 0; j < TX; ++j) {
                     if (j + 1 < TX) fx[(j + 1) & 1] = frag(lx, j + 1);
@@ -340,8 +363,6 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
                 // fences keep that order: left alone, the compiler waits for each product to add it at once.
                 f32x4_t p[2][TY];
                 float sx[2][4];
-                Frag<kPrecise> fx[2];
-                fx[0] = frag(lx, 0);
 #pragma unroll
                 for (int j = 0; j <= TX; ++j) {
                     if (j + 1 < TX) fx[(j + 1) & 1] = frag(lx, j + 1);
