@@ -86,14 +86,14 @@ struct Operand {
 
 // ---------------------------------------------------------------- tiles
 
-// Inclusive prefix sum of v over the wave.
+// Inclusive prefix sum of v over the wave: within rows of 16 lanes, then the rows' sums handed on.
 __device__ __forceinline__ int wave_inclusive(int v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // from 1 lane below in the row
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next, rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
     return v;
 }
 
@@ -170,14 +170,17 @@ __device__ __forceinline__ bool find_tile(const Shape& s, uint32_t item, Tile& t
             return true;
         }
         const int lane = threadIdx.x & 63;
-        uint32_t total = 0;
-        for (int i = 0; i < s.groups; i += 64)
+        int n = group_tiles<BY>(s.offsets, lane, s.groups, s.rows), upto = wave_inclusive(n);
+        uint32_t total = __builtin_amdgcn_readlane(upto, 63);
+        for (int i = 64; i < s.groups; i += 64)
             total += __builtin_amdgcn_readlane(wave_inclusive(group_tiles<BY>(s.offsets, i + lane, s.groups, s.rows)), 63);
         if (!of_all(total * s.xtiles, t)) return false;
         uint32_t before = 0;
         for (int i = 0; i < s.groups; i += 64) {
-            const int n = group_tiles<BY>(s.offsets, i + lane, s.groups, s.rows);
-            const int upto = wave_inclusive(n);
+            if (i > 0) {
+                n = group_tiles<BY>(s.offsets, i + lane, s.groups, s.rows);
+                upto = wave_inclusive(n);
+            }
             const uint64_t past = __ballot((before + upto) * s.xtiles > t);
             if (past) {
                 const int l = __builtin_ctzll(past);
@@ -216,10 +219,17 @@ __device__ __forceinline__ void copy_to_lds4(buffer_t from, uint32_t lane_offset
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_ptr_t)to, 4, lane_offset, offset, 0, 0);
 }
 
+// Waits until at most N of this wave's copies are under way, then for all waves.  What the waves have copied until
+// then can be read, and what they have read can be overwritten.
+template <int N>
+__device__ __forceinline__ void wait_copies_and_meet() {
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
 // Both operands through LDS: tiles of BY x BX outputs, waves WY x WX, one block of 128 a step.  While a step is
-// computed the next one's operands are copied to the other half of LDS.  A row's eight 16-byte parts are kept in the
+// computed the operands of the next STAGES - 1 are copied to other parts of LDS.  A row's eight 16-byte parts are kept in the
 // order part ^ (row % 8), so that the 16 rows that a fragment reads lie in different banks.
-template <int BY, int BX, int WY, int WX, int KIND, bool WGRAD, int OUT>
+template <int BY, int BX, int WY, int WX, int STAGES, int KIND, bool WGRAD, int OUT>
 __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X, Shape shape, void* __restrict__ out) {
     constexpr int NW = WY * WX, TY = BY / WY / 16, TX = BX / WX / 16;  // waves; 16 x 16 tiles of a wave
     constexpr bool kPrecise = OUT == kDtF32;
@@ -230,8 +240,8 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
     constexpr int kScaleRows = BY + (WGRAD ? BX : (BX + kF8Block - 1) / kF8Block);
     constexpr int kScaleStage = (kScaleRows + 3) / 4 * 16 * kSS;  // four blocks' scales of each row
     static_assert(kCopies * NW * 8 == BY + BX && BX / WX <= kF8Block && BY % 64 == 0, "whole copies, and one x scale a wave");
-    __shared__ __align__(1024) uint8_t lds[2 * kStage + 2 * kScaleStage];
-    uint8_t* const lds_scale = lds + 2 * kStage;
+    __shared__ __align__(1024) uint8_t lds[STAGES * kStage + 2 * kScaleStage];
+    uint8_t* const lds_scale = lds + STAGES * kStage;
 
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -260,11 +270,11 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
             else
                 from[i] = min(r - BY, xlast) * static_cast<uint32_t>(X.row_bytes) + part;
         }
-        const auto copy = [&](int kb, int half) {
+        const auto copy_some = [&](int kb, int stage, int i0, int i1) {
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i)
+            for (int i = i0; i < i1; ++i)
                 copy_to_lds16(wave * kCopies + i < BY / 8 ? ybuf : xbuf, from[i], kb * kF8Block,
-                              lds + half * kStage + (wave * kCopies + i) * 1024);
+                              lds + stage * kStage + (wave * kCopies + i) * 1024);
         };
         const buffer_t ysbuf = make_buffer(Y.scales + t.y0 * Y.scale_bytes);
         const int xsrow0 = WGRAD ? x0 : x0 / kF8Block, xslast = (WGRAD ? shape.nx : xblocks) - 1 - xsrow0;
@@ -296,17 +306,25 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
             for (int j = 0; j < TX; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         const bool busy = t.y0 + wy * TY * 16 < t.yend && x0 + wx * TX * 16 < shape.nx;
 
-        if (t.kb0 < t.kb1) {
-            copy(t.kb0, 0);
-            copy_scales(t.kb0 >> 2, (t.kb0 >> 2) & 1);
-        }
+        const auto copy = [&](int kb, int stage) { copy_some(kb, stage, 0, kCopies); };
+        // Block kb's operands into a stage; the scales of its four blocks come with the first of them, before them.
+        const auto copy_step = [&](int kb, int stage) {
+            if ((kb & 3) == 0 || kb == t.kb0) copy_scales(kb >> 2, (kb >> 2) & 1);
+            copy(kb, stage);
+        };
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s)
+            if (t.kb0 + s < t.kb1) copy_step(t.kb0 + s, s);
+        int stage = 0;
         for (int kb = t.kb0; kb < t.kb1; ++kb) {
-            const int half = (kb - t.kb0) & 1;
-            __syncthreads();  // this step's operands are there, and the last step's have been read
-            if (kb + 1 < t.kb1) {
-                copy(kb + 1, half ^ 1);
-                if (((kb + 1) & 3) == 0) copy_scales((kb + 1) >> 2, ((kb + 1) >> 2) & 1);
-            }
+            // This step's copies are the oldest; those of the STAGES - 2 steps after it may still be under way.
+            if (kb + STAGES - 1 <= t.kb1)
+                wait_copies_and_meet<kCopies*(STAGES - 2)>();
+            else
+                wait_copies_and_meet<0>();
+            if (kb + STAGES - 1 < t.kb1) copy_step(kb + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+            const int half = stage;
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
             if (!busy) continue;
             const uint8_t* const ly = lds + half * kStage + wy * TY * 16 * kF8Block;
             const uint8_t* const lx = lds + half * kStage + (BY + wx * TX * 16) * kF8Block;
@@ -392,7 +410,7 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
                 }
             }
         }
-        __syncthreads();  // the last step's operands have been read
+        wait_copies_and_meet<0>();  // the last step's operands have been read
         // Four outputs of a lane lie together.
         constexpr int ES = Arith<OUT>::kEsize;
         const bool whole = (shape.nx & 3) == 0;
@@ -419,34 +437,159 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
     }
 }
 
-template <int BY, int BX, int WY, int WX, bool WGRAD>
-hipError_t launch_tiles(const Operand& Y, const Operand& X, Shape shape, void* out, int kind, int out_dtype,
-                        hipStream_t stream) {
+// ---------------------------------------------------------------- few rows
+
+// 16 bytes twice of a lane's part of a block.
+__device__ __forceinline__ void load_part(const uint8_t* p, i32x4_t (&v)[2]) {
+    v[0] = *reinterpret_cast<const i32x4_t*>(p);
+    v[1] = *reinterpret_cast<const i32x4_t*>(p + 64);
+}
+
+// Few rows: 16 YT rows x 16 XT columns of a workgroup, whose W waves split the blocks among them and add their sums
+// through LDS.  Every byte of the weights is read by one wave, straight into the registers that the products take it
+// from, kAhead blocks at a time; there is nothing for LDS to share.
+template <int YT, int XT, int W, int KIND, int OUT>
+__global__ __launch_bounds__(W * 64) void k_f8_few(Operand Y, Operand X, Shape shape, void* __restrict__ out) {
+    constexpr bool kPrecise = OUT == kDtF32;
+    constexpr bool kScaledOp = KIND == kScaleE8m0 && !kPrecise;
+    constexpr int kAhead = YT + XT <= 2 ? 8 : YT + XT <= 5 ? 2 : 1;
+    constexpr int kRows = 16 * YT, kCols = 16 * XT, kPitch = kCols + 4;  // of the sums in LDS
+    __shared__ float sums[W][kRows][kPitch];
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (int item = blockIdx.x; item < shape.items; item += gridDim.x) {
+        Tile t;
+        if (!find_tile<kRows, false>(shape, item, t)) continue;
+        const int x0 = t.xt * kCols;
+        const int xblocks = (shape.nx + kF8Block - 1) / kF8Block;
+        const int per = (shape.blocks + W - 1) / W;
+        const int kb0 = wave * per, kb1 = min(kb0 + per, shape.blocks);
+        const uint8_t *py[YT], *px[XT], *ps[YT];
+#pragma unroll
+        for (int i = 0; i < YT; ++i) {
+            const int64_t y = min(t.y0 + i * 16 + l16, t.yend - 1);
+            py[i] = Y.values + y * Y.row_bytes + quad * 16;
+            ps[i] = Y.scales + y * Y.scale_bytes;
+        }
+#pragma unroll
+        for (int j = 0; j < XT; ++j)
+            px[j] = X.values + (static_cast<int64_t>(t.g) * shape.nx + min(x0 + j * 16 + l16, shape.nx - 1)) * X.row_bytes + quad * 16;
+        const uint8_t* const pxs = X.scales + (static_cast<int64_t>(t.g) * xblocks + x0 / kF8Block) * X.scale_bytes;
+        f32x4_t acc[YT][XT];
+#pragma unroll
+        for (int i = 0; i < YT; ++i)
+#pragma unroll
+            for (int j = 0; j < XT; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int kb = kb0; kb < kb1; kb += kAhead) {
+            i32x4_t vx[kAhead][XT][2], vy[kAhead][YT][2];
+            uint32_t sy[kAhead][YT], sx[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t k = min(kb + u, kb1 - 1);
+#pragma unroll
+                for (int j = 0; j < XT; ++j) load_part(px[j] + k * kF8Block, vx[u][j]);
+#pragma unroll
+                for (int i = 0; i < YT; ++i) {
+                    load_part(py[i] + k * kF8Block, vy[u][i]);
+                    sy[u][i] = KIND == kScaleF32 ? reinterpret_cast<const uint32_t*>(ps[i])[k] : ps[i][k];
+                }
+                sx[u] = KIND == kScaleF32 ? reinterpret_cast<const uint32_t*>(pxs)[k] : pxs[k];
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (kb + u >= kb1) break;
+#pragma unroll
+                for (int i = 0; i < YT; ++i) {
+                    const Frag<kPrecise> fy = make_frag<kPrecise>(vy[u][i][0], vy[u][i][1]);
+#pragma unroll
+                    for (int j = 0; j < XT; ++j) {
+                        const Frag<kPrecise> fx = make_frag<kPrecise>(vx[u][j][0], vx[u][j][1]);
+                        if constexpr (kScaledOp) {
+                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx.v, fy.v, acc[i][j], 0, 0, 0, sx[u], 0,
+                                                                                         sy[u][i]);
+                        } else {
+                            const float s = KIND == kScaleF32 ? __uint_as_float(sy[u][i]) * __uint_as_float(sx[u])
+                                                              : e8m0_value(sy[u][i]) * e8m0_value(sx[u]);
+                            const f32x4_t p = block_sum<kPrecise>(fx, fy);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(p[r], s, acc[i][j][r]);
+                        }
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < YT; ++i)
+#pragma unroll
+            for (int j = 0; j < XT; ++j)
+                *reinterpret_cast<f32x4_t*>(&sums[wave][i * 16 + l16][j * 16 + quad * 4]) = acc[i][j];
+        __syncthreads();
+        for (int o = tid; o < kRows * kCols; o += W * 64) {
+            const int y = o / kCols, x = o % kCols;
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) v += sums[w][y][x];
+            if (t.y0 + y < t.yend && x0 + x < shape.nx)
+                Arith<OUT>::store1(out, static_cast<int64_t>(t.y0 + y) * shape.nx + x0 + x, v);
+        }
+        __syncthreads();
+    }
+}
+
+// Fills in the tiles of BY x BX outputs and the workgroups that they need at most; false where they are too many to
+// number (more outputs than the memory holds).
+template <int BY, int BX, bool WGRAD>
+bool lay_out(Shape& shape) {
     const int64_t xtiles = (static_cast<int64_t>(shape.nx) + BX - 1) / BX;
     // A group's last tile may be part full: at most one more tile a group that has a row.
     const int64_t ytiles = WGRAD ? (static_cast<int64_t>(shape.ny) + BY - 1) / BY * shape.groups
                                  : shape.offsets ? shape.ny / BY + std::min(shape.groups, shape.ny)
-                                                 : (shape.ny + BY - 1) / BY;
+                                                 : (static_cast<int64_t>(shape.ny) + BY - 1) / BY;
     const int64_t items = (ytiles * xtiles + 7) / 8 * 8;
-    if (items > INT32_MAX - (1 << 20)) return hipErrorInvalidValue;  // more outputs than the memory holds
     shape.xtiles = static_cast<int>(xtiles);
     shape.items = static_cast<int>(items);
-    const int64_t grid = std::min(items, grid_limit(int64_t(1) << 20));
-    const auto go = [&](auto kd, auto od) {
-        k_f8_tiles<BY, BX, WY, WX, decltype(kd)::value, WGRAD, decltype(od)::value>
-            <<<static_cast<uint32_t>(grid), WY * WX * 64, 0, stream>>>(Y, X, shape, out);
-    };
+    return items <= INT32_MAX - (1 << 20);
+}
+
+// f(scale kind, output type) with both as types.
+template <class F>
+void by_kind(int kind, int out_dtype, F f) {
     const auto typed = [&](auto kd) {
         if (out_dtype == kDtBf16)
-            go(kd, std::integral_constant<int, kDtBf16>{});
+            f(kd, std::integral_constant<int, kDtBf16>{});
         else
-            go(kd, std::integral_constant<int, kDtF32>{});
+            f(kd, std::integral_constant<int, kDtF32>{});
     };
     if (kind == kScaleF32)
         typed(std::integral_constant<int, kScaleF32>{});
     else
         typed(std::integral_constant<int, kScaleE8m0>{});
+}
+
+template <int BY, int BX, int WY, int WX, int STAGES, bool WGRAD>
+hipError_t launch_tiles(const Operand& Y, const Operand& X, Shape shape, void* out, int kind, int out_dtype,
+                        hipStream_t stream) {
+    if (!lay_out<BY, BX, WGRAD>(shape)) return hipErrorInvalidValue;
+    const int64_t grid = std::min<int64_t>(shape.items, grid_limit(int64_t(1) << 20));
+    by_kind(kind, out_dtype, [&](auto kd, auto od) {
+        if constexpr (decltype(od)::value == kDtBf16 || BY * BX < 256 * 256)
+            k_f8_tiles<BY, BX, WY, WX, STAGES, decltype(kd)::value, WGRAD, decltype(od)::value>
+                <<<static_cast<uint32_t>(grid), WY * WX * 64, 0, stream>>>(Y, X, shape, out);
+    });
     note_launch(WGRAD ? "k_f8_tiles_wgrad" : "k_f8_tiles", kMapLinear, 1, grid, WY * WX * 64, 1);
+    return hipGetLastError();
+}
+
+template <int YT, int XT, int W>
+hipError_t launch_few(const Operand& Y, const Operand& X, Shape shape, void* out, int kind, int out_dtype,
+                      hipStream_t stream) {
+    if (!lay_out<16 * YT, 16 * XT, false>(shape)) return hipErrorInvalidValue;
+    const int64_t grid = std::min<int64_t>(shape.items, grid_limit(int64_t(1) << 20));
+    by_kind(kind, out_dtype, [&](auto kd, auto od) {
+        k_f8_few<YT, XT, W, decltype(kd)::value, decltype(od)::value>
+            <<<static_cast<uint32_t>(grid), W * 64, 0, stream>>>(Y, X, shape, out);
+    });
+    note_launch("k_f8_few", kMapLinear, 1, grid, W * 64, 1);
     return hipGetLastError();
 }
 
@@ -460,8 +603,37 @@ hipError_t launch_f8_matmul(const void* a, const void* a_scale, const void* b, c
     const Operand X = {static_cast<const uint8_t*>(b), static_cast<const uint8_t*>(b_scale), k, scale_bytes};
     const Shape shape = {offsets, groups, static_cast<int>(rows), static_cast<int>(rows), static_cast<int>(n),
                          static_cast<int>(k / kF8Block), 0, 0};
-    if (rows / groups > 128) return launch_tiles<256, 256, 4, 2, false>(Y, X, shape, out, kind, out_dtype, stream);
-    return launch_tiles<64, 128, 2, 2, false>(Y, X, shape, out, kind, out_dtype, stream);
+    // Which kernel, by the rows of a group (on average, with what the caller has room for) and the number of tiles.
+    // Measured on MI355X, k = 7168 and n = 4096 where nothing else is said, us.  A larger tile moves less through the
+    // L2 and LDS for each product, as long as there are tiles for the 256 compute units; tiles of few rows leave the
+    // matrix units idle but read the weights once all the same.
+    //   256 x 256     dense 4096 rows 99 (128 x 256: 108); 32 groups of 128 rows 226 (232); 256 groups of 128 rows of
+    //                 2048 x 2048 304 (315), of 64 rows 260 (238); dense 2048 rows, 128 tiles, 84 (59)
+    //   128 x 256     dense 2048 rows 59 (64 x 128: 92); 1024 rows, 128 tiles, 50 (47); 32 groups of 64 rows of k = 4096
+    //                 130 (134), of 32 rows 127 (117).  The largest for fp32 results, whose widened fragments do not
+    //                 fit beside 256 x 256 sums: dense 8192^3 964, with 128 x 128 tiles 994
+    //   64 x 128      dense 1024 rows 47 (64 x 64: 63); 512 rows, 256 tiles, 37 (32)
+    //   64 x 64       dense 256 rows 27 (64 x 128: 35); 128 rows 25 (few rows, 32 x 64: 26); 64 rows 24 (few: 17)
+    //   few rows      1 row 9, 16 rows 10, 32 rows 13 (64 x 64: 22); 32 groups of 2 rows 135 (138), of 8 rows 163 (160)
+    const auto tiles = [&](int64_t by, int64_t bx) {
+        const int64_t y = offsets ? rows / by + std::min<int64_t>(groups, rows) : (rows + by - 1) / by;
+        return y * ((n + bx - 1) / bx);
+    };
+    const int64_t each = rows / groups;
+    if (each >= 128 && tiles(256, 256) >= 192 && out_dtype == kDtBf16)
+        return launch_tiles<256, 256, 4, 2, 2, false>(Y, X, shape, out, kind, out_dtype, stream);
+    if (each >= 64 && tiles(128, 256) >= 192)
+        return launch_tiles<128, 256, 2, 4, 3, false>(Y, X, shape, out, kind, out_dtype, stream);
+    if (each <= 4 || (each <= 64 && tiles(64, 64) <= 128)) {
+        if (each <= 16) {
+            if (tiles(16, 64) >= 448) return launch_few<1, 4, 4>(Y, X, shape, out, kind, out_dtype, stream);
+            return launch_few<1, 1, 8>(Y, X, shape, out, kind, out_dtype, stream);
+        }
+        if (each <= 32) return launch_few<1, 2, 8>(Y, X, shape, out, kind, out_dtype, stream);
+        return launch_few<2, 2, 8>(Y, X, shape, out, kind, out_dtype, stream);
+    }
+    if (tiles(64, 128) >= 512) return launch_tiles<64, 128, 2, 2, 3, false>(Y, X, shape, out, kind, out_dtype, stream);
+    return launch_tiles<64, 64, 2, 2, 4, false>(Y, X, shape, out, kind, out_dtype, stream);
 }
 
 hipError_t launch_f8_wgrad(const void* a, const void* a_scale, const void* b, const void* b_scale,
@@ -472,7 +644,7 @@ hipError_t launch_f8_wgrad(const void* a, const void* a_scale, const void* b, co
     const Operand Y = {static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(a_scale), width, scale_bytes};
     const Operand X = {static_cast<const uint8_t*>(b), static_cast<const uint8_t*>(b_scale), width, scale_bytes};
     const Shape shape = {offsets, groups, static_cast<int>(rows), static_cast<int>(n), static_cast<int>(k), 0, 0, 0};
-    return launch_tiles<128, 128, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
+    return launch_tiles<128, 128, 2, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
 }
 
 }  // namespace nuna
