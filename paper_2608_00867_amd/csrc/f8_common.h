@@ -1,5 +1,5 @@
-// f8_common.h -- device helpers of the 8-bit kernels: the quantisation rule,
-// and where a group's rows lie.
+// f8_common.h -- device helpers of the expert layer's kernels: stores of any
+// alignment, the quantisation rule, and where a group's rows lie.
 #pragma once
 
 #include "device_common.h"
@@ -7,6 +7,16 @@
 
 namespace nuna {
 namespace {
+
+// 16 bytes to an address aligned to the elements only; NT: streamed past the caches' other contents.
+template <bool NT>
+__device__ __forceinline__ void store16_any(char* p, const uint4& v) {
+    const u32x4_any_t t = {v.x, v.y, v.z, v.w};
+    if constexpr (NT)
+        __builtin_nontemporal_store(t, reinterpret_cast<u32x4_any_t*>(p));
+    else
+        *reinterpret_cast<u32x4_any_t*>(p) = t;
+}
 
 // ---------------------------------------------------------------- quantisation
 

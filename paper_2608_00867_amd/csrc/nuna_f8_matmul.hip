@@ -251,6 +251,7 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
     for (int item = blockIdx.x; item < shape.items; item += gridDim.x) {
         Tile t;
         if (!find_tile<BY, WGRAD>(shape, item, t)) continue;
+        wait_copies_and_meet<0>();  // the last tile's outputs have left LDS
         const int x0 = t.xt * BX;
         const int64_t xrow0 = WGRAD ? 0 : static_cast<int64_t>(t.g) * shape.nx;
         const int xblocks = (shape.nx + kF8Block - 1) / kF8Block;
@@ -410,28 +411,45 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
                 }
             }
         }
-        wait_copies_and_meet<0>();  // the last step's operands have been read
-        // Four outputs of a lane lie together.
-        constexpr int ES = Arith<OUT>::kEsize;
-        const bool whole = (shape.nx & 3) == 0;
+        wait_copies_and_meet<0>();  // the last step's operands have been read: LDS is free
+        if (!busy) continue;
+        // A wave turns its outputs in LDS, 16 rows at a time, so that a store takes whole lines of a row.
+        constexpr int ES = Arith<OUT>::kEsize, kRowBytes = TX * 16 * ES, kStrip = kRowBytes + 16;
+        static_assert(NW * 16 * kStrip <= STAGES * kStage, "the strips fit");
+        uint8_t* const strip = lds + wave * 16 * kStrip;
+        int el = lane;  // opaque, so that no address of this part is formed, and held, before the loop over the blocks
+        asm volatile("" : "+v"(el));
+        const int xw = x0 + wx * TX * 16, yw = t.y0 + wy * TY * 16, rows_left = t.yend - yw;
+        const int64_t out_row = static_cast<int64_t>(shape.nx) * ES;
+        char* const to = static_cast<char*>(out) + (WGRAD ? static_cast<int64_t>(t.g) * shape.ny + yw : yw) * out_row + xw * ES;
+        const bool whole = xw + TX * 16 <= shape.nx;
 #pragma unroll
         for (int i = 0; i < TY; ++i) {
-            const int y = t.y0 + (wy * TY + i) * 16 + l16;
-            if (y >= t.yend) continue;
-            char* const row = static_cast<char*>(out) + ((WGRAD ? static_cast<int64_t>(t.g) * shape.ny : 0) + y) * shape.nx * ES;
 #pragma unroll
             for (int j = 0; j < TX; ++j) {
-                const int x = x0 + (wx * TX + j) * 16 + quad * 4;
-                if (x + 4 <= shape.nx && whole) {
-                    if constexpr (OUT == kDtF32)
-                        *reinterpret_cast<f32x4_t*>(row + x * ES) = acc[i][j];
-                    else
-                        *reinterpret_cast<uint2*>(row + x * ES) =
-                            make_uint2(f32_to_bf16x2(acc[i][j][0], acc[i][j][1]), f32_to_bf16x2(acc[i][j][2], acc[i][j][3]));
-                } else {
-                    for (int r = 0; r < 4; ++r)
-                        if (x + r < shape.nx) Arith<OUT>::store1(row, x + r, acc[i][j][r]);
+                uint8_t* const at = strip + (el & 15) * kStrip + (j * 16 + (el >> 4) * 4) * ES;
+                if constexpr (OUT == kDtF32)
+                    *reinterpret_cast<f32x4_t*>(at) = acc[i][j];
+                else
+                    *reinterpret_cast<uint2*>(at) =
+                        make_uint2(f32_to_bf16x2(acc[i][j][0], acc[i][j][1]), f32_to_bf16x2(acc[i][j][2], acc[i][j][3]));
+            }
+            if (whole) {
+                constexpr int kLanes = kRowBytes / 16, kAtOnce = 64 / kLanes;  // lanes of a row, rows of a store
+                const int r0 = el / kLanes, at = el % kLanes * 16;
+#pragma unroll
+                for (int r = 0; r < 16; r += kAtOnce) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(strip + (r0 + r) * kStrip + at);
+                    if (i * 16 + r0 + r < rows_left) store16_any<WGRAD>(to + (i * 16 + r0 + r) * out_row + at, v);
                 }
+            } else {
+                using Raw = typename Arith<OUT>::Raw;
+                const int left = shape.nx - xw;
+#pragma nounroll
+                for (int r = 0; r < min(16, rows_left - i * 16); ++r)
+#pragma nounroll
+                    for (int x = el; x < left; x += 64)
+                        reinterpret_cast<Raw*>(to + (i * 16 + r) * out_row)[x] = reinterpret_cast<const Raw*>(strip + r * kStrip)[x];
             }
         }
     }

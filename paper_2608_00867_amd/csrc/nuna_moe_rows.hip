@@ -10,17 +10,10 @@
 // within one workgroup.  They move bytes and are bound by HBM.
 #include <algorithm>
 
-#include "device_common.h"
-#include "expert_kernels.h"
+#include "f8_common.h"
 
 namespace nuna {
 namespace {
-
-// 16 bytes at an address aligned to the elements only.
-__device__ __forceinline__ void store16_any(char* p, const uint4& v) {
-    const u32x4_any_t t = {v.x, v.y, v.z, v.w};
-    *reinterpret_cast<u32x4_any_t*>(p) = t;
-}
 
 template <int DT>
 __device__ __forceinline__ float load1(const char* p) {
@@ -57,7 +50,7 @@ __global__ __launch_bounds__(WG) void k_moe_gather(const char* __restrict__ x, i
             batch_rows(row_of, token, topk, j0, cap, rows);
 #pragma unroll
             for (int j = 0; j < kRowBatch; ++j)
-                if (rows[j] >= 0) store16_any(y + (static_cast<int64_t>(rows[j]) * row_elems + c) * ES, v);
+                if (rows[j] >= 0) store16_any<false>(y + (static_cast<int64_t>(rows[j]) * row_elems + c) * ES, v);
         }
     } else {
         using Raw = typename Arith<DT>::Raw;
@@ -107,7 +100,7 @@ __global__ __launch_bounds__(WG) void k_moe_scatter(const char* __restrict__ y, 
                     Arith<DT>::add(acc, v[j]);
             }
         }
-        store16_any(dst, Arith<DT>::narrow(acc));
+        store16_any<false>(dst, Arith<DT>::narrow(acc));
     } else {
         for (int64_t i = c; i < row_elems; ++i) {
             float acc = 0.0f;
@@ -161,7 +154,7 @@ __global__ __launch_bounds__(kWG) void k_moe_scatter_grad(const char* __restrict
                         dot[j] = fmaf(g[i], b[i], dot[j]);
                         d[i] = w[j] * g[i];
                     }
-                    store16_any(dy + (static_cast<int64_t>(rows[j]) * row_elems + c) * ES, Arith<DT>::narrow(d));
+                    store16_any<false>(dy + (static_cast<int64_t>(rows[j]) * row_elems + c) * ES, Arith<DT>::narrow(d));
                 }
             } else {
                 for (int64_t i = c; i < row_elems; ++i) {
