@@ -124,23 +124,31 @@ __global__ __launch_bounds__(kWG) void k_f8_blocks(const char* __restrict__ x, i
 
 // ---------------------------------------------------------------- columns
 
-// Work item: 64 dwords of columns (128 of bf16, 64 of fp32) of the 128 rows of one block of a group.  The rows go to
-// LDS as they lie, then thread (c, q) takes the column dword c of the rows 32 q .. 32 q + 31.  Row r's dwords are
-// turned by 16 (r / 32), so the four quarters of a column, which neighbouring lanes read, lie in other banks.
-template <int DT, int KIND>
-__global__ __launch_bounds__(kWG) void k_f8_cols(const char* __restrict__ x, int64_t x_stride, int64_t x_rows,
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+
+// Work item: the 128 rows of one block of a group, `span` chunks of 64 dwords of columns (128 of bf16, 64 of fp32).
+// The rows of a chunk go to LDS as they lie, then thread (c, q) takes the column dword c of the rows 16 q .. 16 q + 15
+// and 64 + 16 q .. 64 + 16 q + 15, so that four lanes write 64 bytes together.  Row r's dwords are turned by
+// 16 (r / 16), so the four lanes of a column, which are neighbours, read other banks.  RAGGED: a row of x may end inside
+// 16 bytes.
+template <int DT, int KIND, bool RAGGED>
+__global__ __launch_bounds__(kWG, 4) void k_f8_cols(const char* __restrict__ x, int64_t x_stride, int64_t x_rows,
                                                  const int32_t* __restrict__ slot_of, int topk,
                                                  const int32_t* __restrict__ offsets, int groups, int64_t rows,
-                                                 int64_t cols, int64_t blocks, int64_t pitch, int chunks, int64_t items,
-                                                 uint8_t* __restrict__ out, void* __restrict__ scale) {
+                                                 int64_t cols, int64_t blocks, int64_t pitch, int span, int spans,
+                                                 int64_t items, uint8_t* __restrict__ out, void* __restrict__ scale) {
     constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
+    using Raw = typename Arith<DT>::Raw;
     constexpr int kPer = 4 / ES;             // columns of a dword
-    constexpr int kCols = 64 * kPer;         // columns of a work item
+    constexpr int kCols = 64 * kPer;         // columns of a chunk
     __shared__ __align__(16) uint32_t tile[kF8Block * 64];
     const int tid = threadIdx.x, lane = tid & 63;
+    const int q = lane & 3, cd = (tid >> 6) * 16 + (lane >> 2);
+    const uint32_t* const mine = tile + q * 16 * 64 + ((cd + 16 * q) & 63);  // this thread's column, its first row
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int64_t block = item / chunks;
-        const int64_t c0 = (item - block * chunks) * kCols;
+        const int64_t block = item / spans;
+        const int64_t from_col = (item - block * spans) * span * kCols;
+        const int64_t to_col = min(from_col + static_cast<int64_t>(span) * kCols, cols);
         // The group of this block: the last whose first block is not past it.
         int g = -1;
         for (int i = 0; i < groups; i += 64) {
@@ -153,58 +161,79 @@ __global__ __launch_bounds__(kWG) void k_f8_cols(const char* __restrict__ x, int
             row0 = from + (block - (from / kF8Block + g)) * kF8Block;
             count = to - row0;
         }
-        // 16 threads a row, 16 rows a pass.
-        const int64_t c = c0 + (tid & 15) * L;
+        // 16 threads a row, 16 rows a pass: the rows of x that this thread reads, below 0 where there is none.
+        int source[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int r = (tid >> 4) + 16 * i;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < count && c < cols) {
-                int64_t from = row0 + r;
-                if (slot_of) {
-                    const int slot = slot_of[from];
-                    from = slot < 0 || slot / topk >= x_rows ? -1 : slot / topk;
-                }
-                if (from >= 0) {
-                    const char* p = x + (from * x_stride + c) * ES;
-                    if (c + L <= cols) {
-                        v = load16_any(p);
-                    } else {
-                        typename Arith<DT>::Raw part[L] = {};
-                        for (int k = 0; c + k < cols; ++k) part[k] = reinterpret_cast<const typename Arith<DT>::Raw*>(p)[k];
-                        v = __builtin_bit_cast(uint4, part);
-                    }
+            source[i] = r < count ? static_cast<int>(row0 + r) : -1;
+            if (slot_of && r < count) {
+                const int slot = slot_of[row0 + r];
+                source[i] = slot < 0 || slot / topk >= x_rows ? -1 : slot / topk;
+            }
+        }
+#pragma nounroll
+        for (int64_t c0 = from_col; c0 < to_col; c0 += kCols) {
+            const int64_t c = c0 + (tid & 15) * L;
+            uint4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = make_uint4(0, 0, 0, 0);
+                if (source[i] >= 0 && c + L <= cols) v[i] = load16_any(x + (source[i] * x_stride + c) * ES);
+            }
+            if (RAGGED && c < cols && c + L > cols) {  // the last of a row's parts, element by element
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (source[i] < 0) continue;
+                    const Raw* const p = reinterpret_cast<const Raw*>(x) + source[i] * x_stride + c;
+                    uint32_t part[4] = {};
+#pragma unroll
+                    for (int k = 0; k < L; ++k)
+                        if (c + k < cols) part[k / kPer] |= static_cast<uint32_t>(__builtin_bit_cast(
+                                              std::conditional_t<ES == 2, uint16_t, uint32_t>, p[k])) << (k % kPer * 16);
+                    v[i] = make_uint4(part[0], part[1], part[2], part[3]);
                 }
             }
-            *reinterpret_cast<uint4*>(&tile[r * 64 + (((tid & 15) * 4 + 16 * (r >> 5)) & 63)]) = v;
-        }
-        __syncthreads();
-        const int q = lane & 3, cd = (tid >> 6) * 16 + (lane >> 2);
-        uint32_t w[32];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) w[i] = tile[(q * 32 + i) * 64 + ((cd + 16 * q) & 63)];
-        __syncthreads();
+            for (int i = 0; i < 8; ++i) {
+                const int r = (tid >> 4) + 16 * i;
+                *reinterpret_cast<uint4*>(&tile[r * 64 + (((tid & 15) * 4 + 16 * (r >> 4)) & 63)]) = v[i];
+            }
+            __syncthreads();
+            uint32_t w[32];
 #pragma unroll
-        for (int h = 0; h < kPer; ++h) {
-            const auto value = [&](int i) {
-                return kPer == 1 ? __uint_as_float(w[i]) : h == 0 ? bf16_lo(w[i]) : bf16_hi(w[i]);
-            };
-            uint32_t m = 0;
+            for (int i = 0; i < 32; ++i) w[i] = mine[((i >> 4) * 64 + (i & 15)) * 64];
+            __syncthreads();
+            // The largest magnitudes as integers, of both columns of a dword at once.
+            u16x2_t both = {0, 0};
+            uint32_t one = 0;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) m = max(m, abs_bits(value(i)));
-            const BlockScale s = block_scale<KIND>(max_quad(m));
-            uint32_t b[8];
+            for (int i = 0; i < 32; ++i) {
+                if constexpr (kPer == 2)
+                    both = __builtin_elementwise_max(both, __builtin_bit_cast(u16x2_t, w[i] & 0x7fff7fffu));
+                else
+                    one = max(one, w[i] & 0x7fffffffu);
+            }
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                b[i] = to_e4m3x4(value(4 * i) * s.r, value(4 * i + 1) * s.r, value(4 * i + 2) * s.r, value(4 * i + 3) * s.r);
-            const int64_t col = c0 + cd * kPer + h;
-            if (col < cols) {
-                uint4* to = reinterpret_cast<uint4*>(out + (col * blocks + block) * kF8Block + q * 32);
-                to[0] = make_uint4(b[0], b[1], b[2], b[3]);
-                to[1] = make_uint4(b[4], b[5], b[6], b[7]);
-                if (q == 0) store_scale<KIND>(scale, col * pitch + block, s.kept);
-                if (block == blocks - 1 && q < pitch - blocks)
-                    store_scale<KIND>(scale, col * pitch + blocks + q, kScaleOne<KIND>);
+            for (int h = 0; h < kPer; ++h) {
+                const auto value = [&](int i) {
+                    return kPer == 1 ? __uint_as_float(w[i]) : h == 0 ? bf16_lo(w[i]) : bf16_hi(w[i]);
+                };
+                const BlockScale s = block_scale<KIND>(max_quad(kPer == 1 ? one : static_cast<uint32_t>(both[h]) << 16));
+                uint32_t b[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    b[i] = to_e4m3x4(value(4 * i) * s.r, value(4 * i + 1) * s.r, value(4 * i + 2) * s.r, value(4 * i + 3) * s.r);
+                const int64_t col = c0 + cd * kPer + h;
+                if (col < cols) {
+                    uint8_t* const to = out + (col * blocks + block) * kF8Block + q * 16;
+                    *reinterpret_cast<uint4*>(to) = make_uint4(b[0], b[1], b[2], b[3]);
+                    *reinterpret_cast<uint4*>(to + 64) = make_uint4(b[4], b[5], b[6], b[7]);
+                    if (q == 0) store_scale<KIND>(scale, col * pitch + block, s.kept);
+                    if (block == blocks - 1 && q < pitch - blocks)
+                        store_scale<KIND>(scale, col * pitch + blocks + q, kScaleOne<KIND>);
+                }
+                __builtin_amdgcn_sched_barrier(0);  // one column at a time
             }
         }
     }
@@ -267,12 +296,22 @@ hipError_t launch_f8_cols(const void* x, int64_t x_stride, int64_t x_rows, const
                           void* scale, int kind, hipStream_t stream) {
     const int64_t width = f8_t_width(rows, groups), blocks = width / kF8Block, pitch = f8_pitch(width);
     const int per = dtype == kDtBf16 ? 128 : 64;
-    const int chunks = static_cast<int>((cols + per - 1) / per);
-    const int64_t items = blocks * chunks, grid = quantize_grid(items);
+    const int64_t chunks = (cols + per - 1) / per;
+    // Chunks of a workgroup, one after another: as many as leave four workgroups for each compute unit.
+    const int span = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(8, blocks * chunks / 1024)));
+    const int spans = static_cast<int>((chunks + span - 1) / span);
+    const int64_t items = blocks * spans, grid = quantize_grid(items);
     by_type(dtype, kind, [&](auto dt, auto k) {
-        k_f8_cols<decltype(dt)::value, decltype(k)::value><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(
-            static_cast<const char*>(x), x_stride, x_rows, slot_of, topk, offsets, groups, rows, cols, blocks, pitch,
-            chunks, items, static_cast<uint8_t*>(out), scale);
+        const auto go = [&](auto ragged) {
+            k_f8_cols<decltype(dt)::value, decltype(k)::value, decltype(ragged)::value>
+                <<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(
+                    static_cast<const char*>(x), x_stride, x_rows, slot_of, topk, offsets, groups, rows, cols, blocks, pitch,
+                    span, spans, items, static_cast<uint8_t*>(out), scale);
+        };
+        if (cols % Arith<decltype(dt)::value>::kLanes)
+            go(std::true_type{});
+        else
+            go(std::false_type{});
     });
     note_launch("k_f8_cols", kMapLinear, 1, grid, kWG, 1);
     return hipGetLastError();

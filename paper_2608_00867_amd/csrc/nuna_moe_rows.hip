@@ -22,7 +22,7 @@ __device__ __forceinline__ float load1(const char* p) {
 
 constexpr int kRowBatch = 8;  // rows of a token handled together
 
-// The rows of kRowBatch choices from j0 on: below 0 where there is none.
+// The rows of kRowBatch choices of a token from j0 on: below 0 where there is none.
 __device__ __forceinline__ void batch_rows(const int32_t* __restrict__ row_of, int64_t token, int topk, int j0,
                                            int64_t cap, int (&rows)[kRowBatch]) {
 #pragma unroll
@@ -32,35 +32,48 @@ __device__ __forceinline__ void batch_rows(const int32_t* __restrict__ row_of, i
     }
 }
 
-// Work item: one pass of WG * 16 bytes of one token's row.
-template <int DT, int WG>
-__global__ __launch_bounds__(WG) void k_moe_gather(const char* __restrict__ x, int64_t x_stride,
-                                                   const int32_t* __restrict__ row_of, int topk, int64_t row_elems,
-                                                   int chunks, int64_t items, char* __restrict__ y, int64_t cap) {
-    constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int64_t token = item / chunks;
-    const int64_t c = ((item - token * chunks) * WG + threadIdx.x) * L;
-    if (c >= row_elems) continue;
-    const char* src = x + (token * x_stride + c) * ES;
-    if (c + L <= row_elems) {
-        const uint4 v = load16_any(src);
-        for (int j0 = 0; j0 < topk; j0 += kRowBatch) {
-            int rows[kRowBatch];
-            batch_rows(row_of, token, topk, j0, cap, rows);
+// A thread's part of the rows: 16 bytes of one token's row, the last part of a row shorter where the row is no whole
+// number of them.  Parts are numbered through all rows, so no thread idles at a row's end.
+struct Part {
+    int64_t token, c;  // token, first element
+    bool whole;
+};
+
+template <int DT>
+__device__ __forceinline__ Part part_of(int64_t item, uint32_t parts, int64_t row_elems) {
+    // Up to 2^32 parts the division takes a few instructions.
+    const int64_t token = item < (int64_t(1) << 32) ? static_cast<uint32_t>(item) / parts : item / parts;
+    const int64_t c = (item - token * parts) * Arith<DT>::kLanes;
+    return {token, c, c + Arith<DT>::kLanes <= row_elems};
+}
+
+template <int DT>
+__global__ __launch_bounds__(kWG) void k_moe_gather(const char* __restrict__ x, int64_t x_stride,
+                                                    const int32_t* __restrict__ row_of, int topk, int64_t row_elems,
+                                                    uint32_t parts, int64_t items, char* __restrict__ y, int64_t cap) {
+    constexpr int ES = Arith<DT>::kEsize;
+    using Raw = typename Arith<DT>::Raw;
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; item < items;
+         item += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        const Part p = part_of<DT>(item, parts, row_elems);
+        const char* const src = x + (p.token * x_stride + p.c) * ES;
+        if (p.whole) {
+            const uint4 v = load16_any(src);
+            for (int j0 = 0; j0 < topk; j0 += kRowBatch) {
+                int rows[kRowBatch];
+                batch_rows(row_of, p.token, topk, j0, cap, rows);
 #pragma unroll
-            for (int j = 0; j < kRowBatch; ++j)
-                if (rows[j] >= 0) store16_any<false>(y + (static_cast<int64_t>(rows[j]) * row_elems + c) * ES, v);
+                for (int j = 0; j < kRowBatch; ++j)
+                    if (rows[j] >= 0) store16_any<false>(y + (static_cast<int64_t>(rows[j]) * row_elems + p.c) * ES, v);
+            }
+        } else {
+            for (int j = 0; j < topk; ++j) {
+                const int r = row_of[p.token * topk + j];
+                if (r < 0 || r >= cap) continue;
+                for (int64_t i = 0; p.c + i < row_elems; ++i)
+                    reinterpret_cast<Raw*>(y)[r * row_elems + p.c + i] = reinterpret_cast<const Raw*>(src)[i];
+            }
         }
-    } else {
-        using Raw = typename Arith<DT>::Raw;
-        for (int j = 0; j < topk; ++j) {
-            const int r = row_of[token * topk + j];
-            if (r < 0 || r >= cap) continue;
-            for (int64_t i = c; i < row_elems; ++i)
-                reinterpret_cast<Raw*>(y)[r * row_elems + i] = reinterpret_cast<const Raw*>(x)[token * x_stride + i];
-        }
-    }
     }
 }
 
@@ -72,178 +85,179 @@ __device__ __forceinline__ void fma16(float (&a)[Arith<DT>::kLanes], const uint4
     for (int i = 0; i < Arith<DT>::kLanes; ++i) a[i] = fmaf(w, b[i], a[i]);
 }
 
-template <int DT, bool WEIGHTED, int WG>
-__global__ __launch_bounds__(WG) void k_moe_scatter(const char* __restrict__ y, const int32_t* __restrict__ row_of,
-                                                    const float* __restrict__ weights, int topk, int64_t row_elems,
-                                                    int chunks, int64_t items, int64_t cap, char* __restrict__ out) {
+template <int DT, bool WEIGHTED>
+__global__ __launch_bounds__(kWG) void k_moe_scatter(const char* __restrict__ y, const int32_t* __restrict__ row_of,
+                                                     const float* __restrict__ weights, int topk, int64_t row_elems,
+                                                     uint32_t parts, int64_t items, int64_t cap, char* __restrict__ out) {
     constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int64_t token = item / chunks;
-    const int64_t c = ((item - token * chunks) * WG + threadIdx.x) * L;
-    if (c >= row_elems) continue;
-    char* dst = out + (token * row_elems + c) * ES;
-    if (c + L <= row_elems) {
-        float acc[L] = {};
-        for (int j0 = 0; j0 < topk; j0 += kRowBatch) {
-            int rows[kRowBatch];
-            uint4 v[kRowBatch];
-            batch_rows(row_of, token, topk, j0, cap, rows);
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; item < items;
+         item += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        const Part p = part_of<DT>(item, parts, row_elems);
+        if (p.whole) {
+            float acc[L] = {};
+            for (int j0 = 0; j0 < topk; j0 += kRowBatch) {
+                int rows[kRowBatch];
+                uint4 v[kRowBatch];
+                float w[kRowBatch];
+                batch_rows(row_of, p.token, topk, j0, cap, rows);
 #pragma unroll
-            for (int j = 0; j < kRowBatch; ++j)
-                if (rows[j] >= 0) v[j] = load16_any(y + (static_cast<int64_t>(rows[j]) * row_elems + c) * ES);
+                for (int j = 0; j < kRowBatch; ++j) {
+                    if (rows[j] < 0) continue;
+                    v[j] = load16_any(y + (static_cast<int64_t>(rows[j]) * row_elems + p.c) * ES);
+                    if constexpr (WEIGHTED) w[j] = weights[p.token * topk + j0 + j];
+                }
 #pragma unroll
-            for (int j = 0; j < kRowBatch; ++j) {
-                if (rows[j] < 0) continue;
-                if constexpr (WEIGHTED)
-                    fma16<DT>(acc, v[j], weights[token * topk + j0 + j]);
-                else
-                    Arith<DT>::add(acc, v[j]);
+                for (int j = 0; j < kRowBatch; ++j) {
+                    if (rows[j] < 0) continue;
+                    if constexpr (WEIGHTED)
+                        fma16<DT>(acc, v[j], w[j]);
+                    else
+                        Arith<DT>::add(acc, v[j]);
+                }
+            }
+            store16_any<false>(out + (p.token * row_elems + p.c) * ES, Arith<DT>::narrow(acc));
+        } else {
+            for (int64_t i = p.c; i < row_elems; ++i) {
+                float acc = 0.0f;
+                for (int j = 0; j < topk; ++j) {
+                    const int r = row_of[p.token * topk + j];
+                    if (r < 0 || r >= cap) continue;
+                    const float v = load1<DT>(y + (r * row_elems + i) * ES);
+                    acc = WEIGHTED ? fmaf(weights[p.token * topk + j], v, acc) : acc + v;
+                }
+                Arith<DT>::store1(out, p.token * row_elems + i, acc);
             }
         }
-        store16_any<false>(dst, Arith<DT>::narrow(acc));
-    } else {
-        for (int64_t i = c; i < row_elems; ++i) {
-            float acc = 0.0f;
-            for (int j = 0; j < topk; ++j) {
-                const int r = row_of[token * topk + j];
-                if (r < 0 || r >= cap) continue;
-                const float v = load1<DT>(y + (r * row_elems + i) * ES);
-                acc = WEIGHTED ? fmaf(weights[token * topk + j], v, acc) : acc + v;
-            }
-            Arith<DT>::store1(out, token * row_elems + i, acc);
-        }
-    }
     }
 }
 
-// One workgroup a token, kRowBatch choices at a time: the dot products stay in the threads' registers and are
-// added over the workgroup at the end, in a fixed order.
-template <int DT>
+// One workgroup a token.  kGradSpan parts of dout stay in a thread's registers while the token's rows pass, one after
+// another; a row's products are added over a wave and kept for each wave and choice in LDS, so the sum of a choice has
+// one order: by thread, then wave, then span of columns.  RAGGED: a row may end inside 16 bytes.
+constexpr int kGradSpan = 4;
+
+template <int DT, bool RAGGED>
 __global__ __launch_bounds__(kWG) void k_moe_scatter_grad(const char* __restrict__ dout, const char* __restrict__ y,
                                                           const int32_t* __restrict__ row_of,
                                                           const float* __restrict__ weights, int topk,
                                                           int64_t row_elems, int64_t tokens, int64_t cap,
                                                           char* __restrict__ dy, float* __restrict__ dw) {
     constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
-    __shared__ float sums[kWG / 64][kRowBatch];
-    for (int64_t token = blockIdx.x; token < tokens; token += gridDim.x)
-    for (int j0 = 0; j0 < topk; j0 += kRowBatch) {
-        int rows[kRowBatch];
-        float w[kRowBatch], dot[kRowBatch];
-        batch_rows(row_of, token, topk, j0, cap, rows);
+    __shared__ float sums[kWG / 64][64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int64_t token = blockIdx.x; token < tokens; token += gridDim.x) {
+        for (int j0 = 0; j0 < topk; j0 += 64) {
+            // Lane j holds choice j0 + j, so that all rows and weights come at once.
+            const bool mine = j0 + lane < topk;
+            const int64_t slot = token * topk + j0 + lane;
+            const int row_j = mine ? row_of[slot] : -1;
+            const float weight_j = mine ? weights[slot] : 0.0f;
+            const uint64_t here = __ballot(row_j >= 0 && row_j < cap);
+            sums[wave][lane] = 0.0f;
+            for (int64_t c0 = 0; here && c0 < row_elems; c0 += kGradSpan * kWG * L) {
+                const char* const dout_c = dout + (token * row_elems + c0 + tid * L) * ES;
+                const int64_t left = row_elems - c0 - tid * L;  // elements from this thread's first part on
+                uint4 g[kGradSpan];
 #pragma unroll
-        for (int j = 0; j < kRowBatch; ++j) {
-            w[j] = rows[j] >= 0 ? weights[token * topk + j0 + j] : 0.0f;
-            dot[j] = 0.0f;
-        }
-        for (int64_t c = threadIdx.x * L; c < row_elems; c += kWG * L) {
-            if (c + L <= row_elems) {
-                float g[L];
-                Arith<DT>::init(g, load16_any(dout + (token * row_elems + c) * ES));
-                uint4 v[kRowBatch];
+                for (int s = 0; s < kGradSpan; ++s)
+                    if ((s * kWG + 1) * L <= left) g[s] = load16_any(dout_c + s * kWG * L * ES);
+                for (uint64_t todo = here; todo; todo &= todo - 1) {
+                    const int j = __builtin_ctzll(todo);
+                    const int64_t row = __builtin_amdgcn_readlane(row_j, j) * row_elems + c0 + tid * L;
+                    const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight_j), j));
+                    const char* const y_c = y + row * ES;
+                    char* const dy_c = dy + row * ES;
+                    uint4 v[kGradSpan];
 #pragma unroll
-                for (int j = 0; j < kRowBatch; ++j)
-                    if (rows[j] >= 0) v[j] = load16_any(y + (static_cast<int64_t>(rows[j]) * row_elems + c) * ES);
+                    for (int s = 0; s < kGradSpan; ++s)
+                        if ((s * kWG + 1) * L <= left) v[s] = load16_any(y_c + s * kWG * L * ES);
+                    float dot = 0.0f;
 #pragma unroll
-                for (int j = 0; j < kRowBatch; ++j) {
-                    if (rows[j] < 0) continue;
-                    float b[L], d[L];
-                    Arith<DT>::init(b, v[j]);
+                    for (int s = 0; s < kGradSpan; ++s) {
+                        if ((s * kWG + 1) * L <= left) {
+                            float a[L], b[L], d[L];
+                            Arith<DT>::init(a, g[s]);
+                            Arith<DT>::init(b, v[s]);
 #pragma unroll
-                    for (int i = 0; i < L; ++i) {
-                        dot[j] = fmaf(g[i], b[i], dot[j]);
-                        d[i] = w[j] * g[i];
+                            for (int i = 0; i < L; ++i) {
+                                dot = fmaf(a[i], b[i], dot);
+                                d[i] = w * a[i];
+                            }
+                            store16_any<true>(dy_c + s * kWG * L * ES, Arith<DT>::narrow(d));
+                        } else if (RAGGED) {
+                            for (int64_t i = s * kWG * L; i < left; ++i) {
+                                const float a = load1<DT>(dout_c + i * ES);
+                                dot = fmaf(a, load1<DT>(y_c + i * ES), dot);
+                                Arith<DT>::store1(dy_c, i, w * a);
+                            }
+                        }
                     }
-                    store16_any<false>(dy + (static_cast<int64_t>(rows[j]) * row_elems + c) * ES, Arith<DT>::narrow(d));
-                }
-            } else {
-                for (int64_t i = c; i < row_elems; ++i) {
-                    const float g = load1<DT>(dout + (token * row_elems + i) * ES);
-#pragma unroll
-                    for (int j = 0; j < kRowBatch; ++j) {
-                        if (rows[j] < 0) continue;
-                        const int64_t at = static_cast<int64_t>(rows[j]) * row_elems + i;
-                        dot[j] = fmaf(g, load1<DT>(y + at * ES), dot[j]);
-                        Arith<DT>::store1(dy, at, w[j] * g);
-                    }
+                    for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
+                    if (lane == 0) sums[wave][j] += dot;
                 }
             }
+            if (!here) {  // the same in all waves
+                if (wave == 0 && mine) dw[slot] = 0.0f;
+                continue;
+            }
+            __syncthreads();
+            if (wave == 0 && mine) {
+                float s = 0.0f;
+                for (int k = 0; k < kWG / 64; ++k) s += sums[k][lane];
+                dw[slot] = s;
+            }
+            __syncthreads();
         }
-#pragma unroll
-        for (int j = 0; j < kRowBatch; ++j) {
-            float s = dot[j];
-            for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
-            if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6][j] = s;
-        }
-        __syncthreads();
-        const int j = threadIdx.x;
-        if (j < kRowBatch && j0 + j < topk) {
-            const int r = row_of[token * topk + j0 + j];
-            float s = 0.0f;
-            for (int k = 0; k < kWG / 64; ++k) s += sums[k][j];
-            dw[token * topk + j0 + j] = r >= 0 && r < cap ? s : 0.0f;
-        }
-        __syncthreads();
     }
 }
 
-// Workgroups of 64 threads while they are fewer than four a compute unit, of 256 beyond.
-bool small_grid(int64_t tokens, int64_t row_elems, int lanes) {
-    return tokens * ((row_elems + kWG * lanes - 1) / (kWG * lanes)) < 1024;
+// One part a thread, in workgroups of 256 threads, or of 64 while those are fewer than four a compute unit; a loop
+// beyond 2^20 workgroups or the caller's cap.
+void parts_grid(int64_t items, int& threads, int64_t& grid) {
+    threads = items < 1024 * kWG ? 64 : kWG;
+    grid = std::min((items + threads - 1) / threads, grid_limit(int64_t(1) << 20));
 }
-
-// One work item a workgroup up to 2^20 workgroups or the caller's cap; a loop beyond.
-int64_t rows_grid(int64_t items) { return std::min(items, grid_limit(int64_t(1) << 20)); }
 
 }  // namespace
 
 hipError_t launch_moe_gather(const void* x, int64_t x_stride, const int32_t* row_of, int64_t tokens, int topk,
                              int64_t row_elems, void* y, int64_t cap, int dtype, hipStream_t stream) {
-    const auto go = [&](auto dt, auto wg) {
-        constexpr int DT = decltype(dt)::value, WG = decltype(wg)::value;
-        const int per = WG * Arith<DT>::kLanes;
-        const int chunks = static_cast<int>((row_elems + per - 1) / per);
-        const int64_t items = tokens * chunks, grid = rows_grid(items);
-        k_moe_gather<DT, WG><<<static_cast<uint32_t>(grid), WG, 0, stream>>>(static_cast<const char*>(x), x_stride, row_of,
-                                                                            topk, row_elems, chunks, items,
-                                                                            static_cast<char*>(y), cap);
-        note_launch("k_moe_gather", kMapLinear, 1, grid, WG, 1);
-    };
-    const auto sized = [&](auto dt) {
-        if (small_grid(tokens, row_elems, Arith<decltype(dt)::value>::kLanes))
-            go(dt, std::integral_constant<int, 64>{});
-        else
-            go(dt, std::integral_constant<int, kWG>{});
+    const auto go = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        const int64_t parts = (row_elems + Arith<DT>::kLanes - 1) / Arith<DT>::kLanes, items = tokens * parts;
+        int threads;
+        int64_t grid;
+        parts_grid(items, threads, grid);
+        k_moe_gather<DT><<<static_cast<uint32_t>(grid), threads, 0, stream>>>(
+            static_cast<const char*>(x), x_stride, row_of, topk, row_elems, static_cast<uint32_t>(parts), items,
+            static_cast<char*>(y), cap);
+        note_launch("k_moe_gather", kMapLinear, 1, grid, threads, 1);
     };
     if (dtype == kDtBf16)
-        sized(std::integral_constant<int, kDtBf16>{});
+        go(std::integral_constant<int, kDtBf16>{});
     else
-        sized(std::integral_constant<int, kDtF32>{});
+        go(std::integral_constant<int, kDtF32>{});
     return hipGetLastError();
 }
 
 hipError_t launch_moe_scatter(const void* y, const int32_t* row_of, const float* weights, int64_t tokens, int topk,
                               int64_t row_elems, int64_t cap, void* out, int dtype, hipStream_t stream) {
-    const auto go = [&](auto dt, auto weighted, auto wg) {
-        constexpr int DT = decltype(dt)::value, WG = decltype(wg)::value;
-        const int per = WG * Arith<DT>::kLanes;
-        const int chunks = static_cast<int>((row_elems + per - 1) / per);
-        const int64_t items = tokens * chunks, grid = rows_grid(items);
-        k_moe_scatter<DT, decltype(weighted)::value, WG><<<static_cast<uint32_t>(grid), WG, 0, stream>>>(
-            static_cast<const char*>(y), row_of, weights, topk, row_elems, chunks, items, cap, static_cast<char*>(out));
-        note_launch("k_moe_scatter", kMapLinear, 1, grid, WG, 1);
-    };
-    const auto sized = [&](auto dt, auto weighted) {
-        if (small_grid(tokens, row_elems, Arith<decltype(dt)::value>::kLanes))
-            go(dt, weighted, std::integral_constant<int, 64>{});
-        else
-            go(dt, weighted, std::integral_constant<int, kWG>{});
+    const auto go = [&](auto dt, auto weighted) {
+        constexpr int DT = decltype(dt)::value;
+        const int64_t parts = (row_elems + Arith<DT>::kLanes - 1) / Arith<DT>::kLanes, items = tokens * parts;
+        int threads;
+        int64_t grid;
+        parts_grid(items, threads, grid);
+        k_moe_scatter<DT, decltype(weighted)::value><<<static_cast<uint32_t>(grid), threads, 0, stream>>>(
+            static_cast<const char*>(y), row_of, weights, topk, row_elems, static_cast<uint32_t>(parts), items, cap,
+            static_cast<char*>(out));
+        note_launch("k_moe_scatter", kMapLinear, 1, grid, threads, 1);
     };
     const auto typed = [&](auto dt) {
         if (weights)
-            sized(dt, std::true_type{});
+            go(dt, std::true_type{});
         else
-            sized(dt, std::false_type{});
+            go(dt, std::false_type{});
     };
     if (dtype == kDtBf16)
         typed(std::integral_constant<int, kDtBf16>{});
@@ -255,11 +269,18 @@ hipError_t launch_moe_scatter(const void* y, const int32_t* row_of, const float*
 hipError_t launch_moe_scatter_grad(const void* dout, const void* y, const int32_t* row_of, const float* weights,
                                    int64_t tokens, int topk, int64_t row_elems, int64_t cap, void* dy, float* dw,
                                    int dtype, hipStream_t stream) {
-    const int64_t grid = rows_grid(tokens);
+    const int64_t grid = std::min(tokens, grid_limit(int64_t(1) << 20));
     const auto go = [&](auto dt) {
-        k_moe_scatter_grad<decltype(dt)::value><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(
-            static_cast<const char*>(dout), static_cast<const char*>(y), row_of, weights, topk, row_elems, tokens, cap,
-            static_cast<char*>(dy), dw);
+        const auto go2 = [&](auto ragged) {
+            k_moe_scatter_grad<decltype(dt)::value, decltype(ragged)::value>
+                <<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(static_cast<const char*>(dout), static_cast<const char*>(y),
+                                                                  row_of, weights, topk, row_elems, tokens, cap,
+                                                                  static_cast<char*>(dy), dw);
+        };
+        if (row_elems % Arith<decltype(dt)::value>::kLanes)
+            go2(std::true_type{});
+        else
+            go2(std::false_type{});
     };
     if (dtype == kDtBf16)
         go(std::integral_constant<int, kDtBf16>{});

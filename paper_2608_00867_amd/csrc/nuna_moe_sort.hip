@@ -91,6 +91,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(const int32_t* __re
                                                              int32_t* __restrict__ row_of) {
     __shared__ int wave_count[kSortWaves][kMaxExperts];  // per wave: slots of each expert, then the next row
     __shared__ int wave_sums[kSortWaves];
+    __shared__ int2 part_sums[ONE ? 1 : kSortThreads];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t base = static_cast<int64_t>(blockIdx.x) * chunk;
     const int span = chunk / kSortWaves;  // whole rounds of 64
@@ -104,14 +105,27 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_place(const int32_t* __re
     __syncthreads();
     // Thread e: slots of expert e in all chunks and in the chunks before this one.
     int all = 0, before = 0;
-    if (tid < experts) {
-        if (ONE) {
+    if constexpr (ONE) {
+        if (tid < experts)
             for (int w = 0; w < kSortWaves; ++w) all += wave_count[w][tid];
-        } else {
-            for (int c = 0; c < chunks; ++c) {
-                const int v = counts[static_cast<int64_t>(c) * experts + tid];
-                all += v;
-                before += c < static_cast<int>(blockIdx.x) ? v : 0;
+    } else {
+        // All threads add: 2^bits of them a row of counts, the rows dealt round the parts; then the parts.
+        const int e = tid & ((1 << bits) - 1), part = tid >> bits, parts = kSortThreads >> bits;
+        int2 sum = make_int2(0, 0);
+        if (e < experts) {
+#pragma unroll 8
+            for (int c = part; c < chunks; c += parts) {
+                const int v = counts[static_cast<int64_t>(c) * experts + e];
+                sum.x += v;
+                sum.y += c < static_cast<int>(blockIdx.x) ? v : 0;
+            }
+        }
+        part_sums[tid] = sum;
+        __syncthreads();
+        if (tid < experts) {
+            for (int q = 0; q < parts; ++q) {
+                all += part_sums[(q << bits) + tid].x;
+                before += part_sums[(q << bits) + tid].y;
             }
         }
     }
