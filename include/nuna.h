@@ -555,8 +555,9 @@ nuna_status_t nuna_f8_quantize_cols(const void* x, int64_t x_stride, size_t x_ro
  *   a  [n][tc] with its scales;  b  [k][tc] with its scales;
  *   out  [groups][n][k] of out_dtype; a group without rows gets zeros.
  *
- * k of nuna_f8_matmul is a multiple of NUNA_F8_BLOCK (NUNA_ERR_UNSUPPORTED
- * otherwise), n any.  Each block of 128 is summed by the matrix instructions
+ * k of nuna_f8_matmul is a multiple of NUNA_F8_BLOCK, n any.  A row of an
+ * operand holds less than 2^24 bytes: k and tc are below 2^24
+ * (NUNA_ERR_UNSUPPORTED otherwise).  Each block of 128 is summed by the matrix instructions
  * in fp32; fp32 scales multiply the block's sum.
  */
 nuna_status_t nuna_f8_matmul(const void* a, const void* a_scale, const void* b, const void* b_scale,

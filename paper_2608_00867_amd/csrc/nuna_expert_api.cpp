@@ -21,6 +21,8 @@ constexpr size_t kMaxBytes = size_t(1) << 48;
 constexpr size_t kMaxRowElems = size_t(1) << 30;
 // Rows are numbered by int32 entries of the device tables.
 constexpr size_t kMaxRows = size_t(1) << 30;
+// Bytes of an 8-bit operand's row at most: the products copy tiles of up to 256 rows at 32-bit offsets from the first.
+constexpr size_t kMaxF8Row = (size_t(1) << 24) - NUNA_F8_BLOCK;
 
 // A buffer of a call: its name, address, bytes and required alignment.
 struct Buffer {
@@ -312,6 +314,7 @@ nuna_status_t nuna_f8_matmul(const void* a, const void* a_scale, const void* b, 
     NUNA_TRY(check_row(n));
     NUNA_TRY(check_row(k));
     if (k % NUNA_F8_BLOCK) return api_fail(NUNA_ERR_UNSUPPORTED, "k=%zu is no multiple of %d", k, NUNA_F8_BLOCK);
+    if (k > kMaxF8Row) return api_fail(NUNA_ERR_UNSUPPORTED, "k=%zu above %zu", k, kMaxF8Row);
     const size_t ss = nuna::f8_scale_size(kind), pitch = f8_pitch(k), n_blocks = (n + NUNA_F8_BLOCK - 1) / NUNA_F8_BLOCK;
     NUNA_TRY(check_buffers({{"a", a, product(rows, k, 1, 1), 16, false},
                             {"a_scale", a_scale, product(rows, pitch, 1, ss), 16, false},
@@ -337,6 +340,8 @@ nuna_status_t nuna_f8_wgrad(const void* a, const void* a_scale, const void* b, c
     NUNA_TRY(check_row(n));
     NUNA_TRY(check_row(k));
     const size_t ss = nuna::f8_scale_size(kind), width = nuna::f8_t_width(rows, groups), pitch = f8_pitch(width);
+    if (width > kMaxF8Row)
+        return api_fail(NUNA_ERR_UNSUPPORTED, "rows=%zu of %d groups: rows of %zu bytes, above %zu", rows, groups, width, kMaxF8Row);
     NUNA_TRY(check_buffers({{"a", a, product(n, width, 1, 1), 16, false},
                             {"a_scale", a_scale, product(n, pitch, 1, ss), 16, false},
                             {"b", b, product(k, width, 1, 1), 16, false},

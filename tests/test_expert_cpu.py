@@ -111,6 +111,19 @@ def test_products_refuse():
 
 
 @no_gpu_only
+def test_products_refuse_rows_past_their_offsets():
+    """Tiles of 256 rows are copied at 32-bit offsets: a row of 2^24 bytes or more would wrap."""
+    most = (1 << 24) - 128
+    far = [BASE + (i << 40) for i in range(6)]
+    good = dict(a=far[0], sa=far[1], b=far[2], sb=far[3], off=None, groups=1, rows=300, n=300, k=most, out=far[5], kind=0,
+                dtype=nuna.BF16, stream=None)
+    refused("nuna_f8_matmul", good, [(dict(k=1 << 24), UNSUPPORTED), (dict(k=1 << 30), UNSUPPORTED)])
+    good = dict(a=far[0], sa=far[1], b=far[2], sb=far[3], off=far[4], groups=8, rows=most - 8 * 128, n=300, k=300,
+                out=far[5], kind=0, dtype=nuna.F32, stream=None)
+    refused("nuna_f8_wgrad", good, [(dict(rows=most - 7 * 128), UNSUPPORTED), (dict(rows=1 << 30), UNSUPPORTED)])
+
+
+@no_gpu_only
 def test_nothing_to_do_needs_no_device():
     L = nuna.lib()
     assert L.nuna_moe_gather(None, 8, None, 0, 2, 8, None, 0, nuna.BF16, None) == nuna.OK
