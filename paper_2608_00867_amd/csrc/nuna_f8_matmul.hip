@@ -235,6 +235,26 @@ __device__ __forceinline__ void wait_copies_and_meet() {
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// N times 16 bytes from LDS.  (Before a read of its own the compiler waits for every copy to LDS under way, and for the
+// stores issued after them.)
+__device__ __forceinline__ uint32_t lds_address(const uint8_t* p) {
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
+}
+template <int N>
+__device__ __forceinline__ void read_lds16(const uint32_t (&at)[N], u32x4_t (&v)[N]) {
+    static_assert(N == 1 || N == 2 || N == 4, "an instruction each");
+    if constexpr (N == 1)
+        asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v[0]) : "v"(at[0]) : "memory");
+    else if constexpr (N == 2)
+        asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]) : "v"(at[0]), "v"(at[1]) : "memory");
+    else
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+                     : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]) : "memory");
+}
+
 // Both operands through LDS: tiles of BY x BX outputs, waves WY x WX, one block of 128 a step.  While a step is
 // computed the operands of the next STAGES - 1 are copied to other parts of LDS.  A row's eight 16-byte parts are kept in the
 // order part ^ (row % 8), so that the 16 rows that a fragment reads lie in different banks.
@@ -436,10 +456,16 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
             if (whole) {
                 constexpr int kLanes = kRowBytes / 16, kAtOnce = 64 / kLanes;  // lanes of a row, rows of a store
                 const int r0 = el / kLanes, at = el % kLanes * 16;
+                uint32_t addr[16 / kAtOnce];
+                u32x4_t v[16 / kAtOnce];
 #pragma unroll
-                for (int r = 0; r < 16; r += kAtOnce) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(strip + (r0 + r) * kStrip + at);
-                    if (i * 16 + r0 + r < rows_left) store16_any<WGRAD>(to + (i * 16 + r0 + r) * out_row + at, v);
+                for (int r = 0; r < 16 / kAtOnce; ++r) addr[r] = lds_address(strip + (r0 + r * kAtOnce) * kStrip + at);
+                read_lds16(addr, v);
+#pragma unroll
+                for (int r = 0; r < 16 / kAtOnce; ++r) {
+                    const int row = i * 16 + r0 + r * kAtOnce;
+                    if (row < rows_left)
+                        store16_any<WGRAD>(to + row * out_row + at, make_uint4(v[r][0], v[r][1], v[r][2], v[r][3]));
                 }
             } else {
                 using Raw = typename Arith<OUT>::Raw;
@@ -658,11 +684,13 @@ hipError_t launch_f8_wgrad(const void* a, const void* a_scale, const void* b, co
     const Operand Y = {static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(a_scale), width, scale_bytes};
     const Operand X = {static_cast<const uint8_t*>(b), static_cast<const uint8_t*>(b_scale), width, scale_bytes};
     const Shape shape = {offsets, groups, static_cast<int>(rows), static_cast<int>(n), static_cast<int>(k), 0, 0, 0};
-    // Of groups of few rows the outputs are most of the work, and two smaller workgroups of a compute unit hide each
-    // other's stores (32 groups of 256 rows, fp32 results 560 us, with 256 x 128 tiles 580); of many rows the larger
-    // tile moves less (8 groups of 4096 rows 492, with 128 x 128 tiles 591).
+    // Of groups of few rows the outputs are most of the work, and two smaller workgroups of a compute unit, of 8 waves
+    // each, hide each other's stores: 32 groups of 256 rows, n = 2048, k = 7168, fp32 results, 587 us, with 4 waves of
+    // 64 x 64 648, with 64 x 128 tiles 648, with 256 x 128 643.  (723 us where the operands' rows are a multiple of
+    // 4 KiB apart: their lines then meet in few of the memory's channels.)  Of many rows the larger tile moves less (8
+    // groups of 4096 rows 492, with 128 x 128 tiles 591).
     if (rows / groups >= 1024) return launch_tiles<256, 128, 4, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
-    return launch_tiles<128, 128, 2, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
+    return launch_tiles<128, 128, 4, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
 }
 
 }  // namespace nuna
