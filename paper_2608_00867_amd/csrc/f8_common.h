@@ -28,6 +28,7 @@ __device__ __forceinline__ void store16_any(char* p, const uint4& v) {
 struct BlockScale {
     uint32_t kept;
     float r;
+    float value;  // a power of two's
 };
 
 template <int KIND>
@@ -39,10 +40,10 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits) {
     const bool finite = amax_bits < 0x7f800000u;
     if constexpr (KIND == kScaleF32) {
         if (!finite) b = 0x7fc00000u;
-        return {b, 1.0f / __uint_as_float(b)};
+        return {b, 1.0f / __uint_as_float(b), 0.0f};
     } else {
         const uint32_t e = finite ? (b + 0x7fffffu) >> 23 : 255u;  // up to the next power of two
-        return {e, __uint_as_float(finite ? (254u - e) << 23 : 0x7fc00000u)};
+        return {e, __uint_as_float(finite ? (254u - e) << 23 : 0x7fc00000u), __uint_as_float(finite ? e << 23 : 0x7fc00000u)};
     }
 }
 
@@ -63,6 +64,16 @@ __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d
     int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     v = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
     return static_cast<uint32_t>(v);
+}
+
+// Four bf16 values, two a dword, divided by a power of two on the way.  The instruction takes the place of the two
+// products and their widening; it rounds once, as the quotient is exact.
+typedef short i16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t bf16_to_e4m3x4(uint32_t ab, uint32_t cd, float scale) {
+    i16x2_t v = {0, 0};
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(v, __builtin_bit_cast(bf16x2_t, ab), scale, false);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(v, __builtin_bit_cast(bf16x2_t, cd), scale, true);
+    return __builtin_bit_cast(uint32_t, v);
 }
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
