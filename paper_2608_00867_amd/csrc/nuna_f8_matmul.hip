@@ -697,8 +697,12 @@ hipError_t launch_f8_wgrad(const void* a, const void* a_scale, const void* b, co
     // each, hide each other's stores: 32 groups of 256 rows, n = 2048, k = 7168, fp32 results, 587 us, with 4 waves of
     // 64 x 64 648, with 64 x 128 tiles 648, with 256 x 128 643.  (723 us where the operands' rows are a multiple of
     // 4 KiB apart: their lines then meet in few of the memory's channels.)  Of many rows the larger tile moves less (8
-    // groups of 4096 rows 492, with 128 x 128 tiles 591).
+    // groups of 4096 rows 492, with 128 x 128 tiles 591).  fp32 scales and fp32 results together take 138 registers, of
+    // which two workgroups of 8 waves do not fit: 4 waves there (784 us in that form, in 8 waves 1065, held to 128
+    // registers 802).
     if (rows / groups >= 1024) return launch_tiles<256, 128, 4, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
+    if (kind == kScaleF32 && out_dtype == kDtF32)
+        return launch_tiles<128, 128, 2, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
     return launch_tiles<128, 128, 4, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
 }
 
