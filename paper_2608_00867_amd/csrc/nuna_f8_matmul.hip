@@ -450,7 +450,7 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
         const int xw = x0 + wx * TX * 16, yw = t.y0 + wy * TY * 16, rows_left = t.yend - yw;
         const int64_t out_row = static_cast<int64_t>(shape.nx) * ES;
         char* const to = static_cast<char*>(out) + (WGRAD ? static_cast<int64_t>(t.g) * shape.ny + yw : yw) * out_row + xw * ES;
-        const bool whole = xw + TX * 16 <= shape.nx;
+        const int row_bytes = min(TX * 16, shape.nx - xw) * ES;  // of the wave's columns that exist
 #pragma unroll
         for (int i = 0; i < TY; ++i) {
 #pragma unroll
@@ -462,28 +462,35 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
                     *reinterpret_cast<uint2*>(at) =
                         make_uint2(f32_to_bf16x2(acc[i][j][0], acc[i][j][1]), f32_to_bf16x2(acc[i][j][2], acc[i][j][3]));
             }
-            if (whole) {
-                constexpr int kLanes = kRowBytes / 16, kAtOnce = 64 / kLanes;  // lanes of a row, rows of a store
-                const int r0 = el / kLanes, at = el % kLanes * 16;
-                uint32_t addr[16 / kAtOnce];
-                u32x4_t v[16 / kAtOnce];
+            constexpr int kLanes = kRowBytes / 16, kAtOnce = 64 / kLanes;  // lanes of a row, rows of a store
+            const int r0 = el / kLanes, at = el % kLanes * 16;
+            uint32_t addr[16 / kAtOnce];
+            u32x4_t v[16 / kAtOnce];
 #pragma unroll
-                for (int r = 0; r < 16 / kAtOnce; ++r) addr[r] = lds_address(strip + (r0 + r * kAtOnce) * kStrip + at);
-                read_lds16(addr, v);
+            for (int r = 0; r < 16 / kAtOnce; ++r) addr[r] = lds_address(strip + (r0 + r * kAtOnce) * kStrip + at);
+            read_lds16(addr, v);
+            // Of a tile whose columns all exist every lane stores; otherwise those of the whole 16-byte parts, and the part
+            // that the row ends in goes element by element.
+            const auto put = [&] {
 #pragma unroll
                 for (int r = 0; r < 16 / kAtOnce; ++r) {
                     const int row = i * 16 + r0 + r * kAtOnce;
                     if (row < rows_left)
                         store16_any<WGRAD>(to + row * out_row + at, make_uint4(v[r][0], v[r][1], v[r][2], v[r][3]));
                 }
-            } else {
+            };
+            if (row_bytes == kRowBytes) {
+                put();
+            } else if (at + 16 <= row_bytes) {
+                put();
+            } else if (at < row_bytes) {
                 using Raw = typename Arith<OUT>::Raw;
-                const int left = shape.nx - xw;
 #pragma nounroll
-                for (int r = 0; r < min(16, rows_left - i * 16); ++r)
+                for (int r = r0; r < min(16, rows_left - i * 16); r += kAtOnce)
 #pragma nounroll
-                    for (int x = el; x < left; x += 64)
-                        reinterpret_cast<Raw*>(to + (i * 16 + r) * out_row)[x] = reinterpret_cast<const Raw*>(strip + r * kStrip)[x];
+                    for (int x = 0; x < row_bytes - at; x += ES)
+                        *reinterpret_cast<Raw*>(to + (i * 16 + r) * out_row + at + x) =
+                            *reinterpret_cast<const Raw*>(strip + r * kStrip + at + x);
             }
         }
     }
@@ -662,8 +669,11 @@ hipError_t launch_f8_matmul(const void* a, const void* a_scale, const void* b, c
     //                 130 (134), of 32 rows 127 (117).  The largest for fp32 results, whose widened fragments do not
     //                 fit beside 256 x 256 sums: dense 8192^3 964, with 128 x 128 tiles 994
     //   64 x 128      dense 1024 rows 47 (64 x 64: 63); 512 rows, 256 tiles, 37 (32)
-    //   64 x 64       dense 256 rows 27 (64 x 128: 35); 128 rows 25 (few rows, 32 x 64: 26); 64 rows 24 (few: 17)
-    //   few rows      1 row 9, 16 rows 10, 32 rows 13 (64 x 64: 22); 32 groups of 2 rows 135 (138), of 8 rows 163 (160)
+    //   64 x 64       dense 256 rows 27 (64 x 128: 35); 128 rows 25 (few rows, 32 x 32: 34)
+    //   few rows      1 row 7, 16 rows 10, 32 rows 13 (64 x 64: 22); 32 groups of 2 rows 135 (138), of 8 rows 163 (160).
+    //                 Tiles of 32 x 32 as long as there is one for each compute unit at most, whatever the rows: 64 rows
+    //                 17 (24); 128 rows of n = 2048, 256 tiles, 18.7 (24.3), 192 rows 34 (25); 256 rows of n = 1024
+    //                 18.7 (24.4); 512 rows of n = 512, k = 2048, 7.4 (9.1)
     const auto tiles = [&](int64_t by, int64_t bx) {
         const int64_t y = offsets ? rows / by + std::min<int64_t>(groups, rows) : (rows + by - 1) / by;
         return y * ((n + bx - 1) / bx);
@@ -673,7 +683,7 @@ hipError_t launch_f8_matmul(const void* a, const void* a_scale, const void* b, c
         return launch_tiles<256, 256, 4, 2, 2, false>(Y, X, shape, out, kind, out_dtype, stream);
     if (each >= 64 && tiles(128, 256) >= 192)
         return launch_tiles<128, 256, 2, 4, 3, false>(Y, X, shape, out, kind, out_dtype, stream);
-    if (each <= 4 || (each <= 64 && tiles(64, 64) <= 128)) {
+    if (each <= 4 || (each <= 32 && tiles(64, 64) <= 128) || tiles(32, 32) <= 256) {
         if (each <= 16) {
             if (tiles(16, 64) >= 448) return launch_few<1, 4, 4>(Y, X, shape, out, kind, out_dtype, stream);
             return launch_few<1, 1, 8>(Y, X, shape, out, kind, out_dtype, stream);

@@ -432,6 +432,35 @@ def test_matmul(nuna, rows, n, k, kind, out):
     check()
 
 
+# One size for each form of the product: (rows, n, k, groups, the kernel).  Odd n, so that rows of out start anywhere and
+# end inside 16 bytes; rows and blocks that end inside a tile.
+FORMS = [(3, 30001, 256, 1, "k_f8_few"), (13, 200, 640, 1, "k_f8_few"), (29, 1001, 1200, 1, "k_f8_few"),
+         (200, 1021, 1300, 1, "k_f8_few"), (300, 2101, 300, 1, "k_f8_tiles"), (640, 4203, 384, 16, "k_f8_tiles"),
+         (1000, 6201, 384, 1, "k_f8_tiles"), (2100, 6201, 600, 1, "k_f8_tiles"), (2500, 5333, 384, 7, "k_f8_tiles")]
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+@pytest.mark.parametrize("rows,n,k,groups,kernel", FORMS)
+def test_every_form_of_the_product(nuna, rows, n, k, groups, kernel, kind, out):
+    cuts = np.sort(np.random.default_rng(rows).integers(0, rows + 1, groups - 1))
+    off = np.concatenate([[0], cuts, [rows]]).astype(np.int32)
+    a, sa, a64 = rows8(nuna, rows, k, kind, n)
+    b, sb, b64 = weights8(nuna, groups, n, k, kind, rows)
+    o, check = guarded(rows, n, DTYPES[out], 0xFF)
+    if groups == 1:
+        nuna.f8_matmul(a, sa, b[0], sb[0], o)
+    else:
+        nuna.f8_matmul(a, sa, b, sb, o, offsets=dev(off))
+    assert nuna.last_launch()["kernels"] == kernel
+    got = host(o)
+    for g in range(groups):
+        r = slice(off[g], off[g + 1])
+        want, size = a64[r] @ b64[g].T, np.abs(a64[r]) @ np.abs(b64[g]).T
+        bounded(got[r], want, product_bound(want, size, k, out), f"out of group {g}")
+    check()
+
+
 MANY = [(1, [1]), (4, [0, 3, 0, 1]), (40, [1] * 40), (70, [5, 0, 64, 1]), (200, [16, 17, 33, 100, 0, 34]), (520, [256, 1, 0, 263]),
         (600, [0, 0, 600]), (1300, [700, 90, 10, 500]), (0, [0, 0])]
 
