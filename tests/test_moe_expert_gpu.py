@@ -509,6 +509,14 @@ def test_wgrad(nuna, rows, counts, n, k, kind, out):
     check()
 
 
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+@pytest.mark.parametrize("n,k", [(300, 203), (513, 130)])
+def test_wgrad_of_many_rows(nuna, n, k, kind, out):
+    """Groups of more than 1024 rows on average, one of them short."""
+    test_wgrad(nuna, 3300, [2100, 7, 1193], n, k, kind, out)
+
+
 def test_gradient_of_the_rows_is_the_product_with_the_transpose(nuna):
     """dx = dy W: the transposed weights' blocks have the same bytes and scales, so quantising before or after the
     transposition is the same."""
