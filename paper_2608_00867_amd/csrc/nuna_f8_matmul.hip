@@ -33,6 +33,7 @@
 #include <algorithm>
 
 #include "f8_common.h"
+#include "tile_order.h"
 
 namespace nuna {
 namespace {
@@ -449,7 +450,8 @@ __global__ __launch_bounds__(WY * WX * 64) void k_f8_tiles(Operand Y, Operand X,
         asm volatile("" : "+v"(el));
         const int xw = x0 + wx * TX * 16, yw = t.y0 + wy * TY * 16, rows_left = t.yend - yw;
         const int64_t out_row = static_cast<int64_t>(shape.nx) * ES;
-        char* const to = static_cast<char*>(out) + (WGRAD ? static_cast<int64_t>(t.g) * shape.ny + yw : yw) * out_row + xw * ES;
+        char* const to = static_cast<char*>(out) +
+                         out_offset(WGRAD ? static_cast<int64_t>(t.g) * shape.ny + yw : yw, xw, shape.nx, ES);
         const int row_bytes = min(TX * 16, shape.nx - xw) * ES;  // of the wave's columns that exist
 #pragma unroll
         for (int i = 0; i < TY; ++i) {

@@ -1,0 +1,43 @@
+"""The expert layer on the GPU at the ends of its ranges: long rows, many groups, edges of the number formats.
+
+Bounds as in test_moe_expert_gpu.py unless a test says otherwise.  This file comes after the tests that pin the map from
+workgroups to XCDs, as that one does."""
+import numpy as np
+import pytest
+
+import expert_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+F8 = torch.float8_e4m3fn
+E8M0 = torch.float8_e8m0fnu
+ONE = 0x38  # 1.0 in e4m3
+
+
+@pytest.fixture(scope="module")
+def nuna():
+    from paper_2608_00867_amd import nuna as n
+    n.init()
+    return n
+
+
+def test_columns_past_2_to_29_of_fp32_results(nuna):
+    """A row of results of more than 2^31 bytes: every column is where it belongs."""
+    torch.cuda.empty_cache()
+    k, width = (1 << 29) + 128, 128
+    b = torch.zeros((k, width), dtype=torch.uint8, device="cuda")
+    for x in (0, 5, (1 << 28) + 3, (1 << 29) - 1, 1 << 29, (1 << 29) + 77, k - 1):
+        b[x, 0] = ONE + x % 7
+    sb = torch.full((k, 4), 127, dtype=torch.uint8, device="cuda")
+    a = torch.zeros((1, width), dtype=torch.uint8, device="cuda")
+    a[0, 0] = ONE
+    sa = torch.full((1, 4), 127, dtype=torch.uint8, device="cuda")
+    off = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    out = torch.full((1, 1, k), float("nan"), device="cuda")
+    nuna.f8_wgrad(a.view(F8), sa.view(E8M0), b.view(F8), sb.view(E8M0), off, out)
+    assert nuna.last_launch()["kernels"] == "k_f8_tiles_wgrad"
+    assert bool((out[0, 0] == b[:, 0].contiguous().view(F8).float()).all())
+    del b, sb, out
+    torch.cuda.empty_cache()
