@@ -137,6 +137,7 @@ struct Shape {
     int rows;    // that the offsets are cut to
     int ny, nx;  // of a product: rows (all groups') and columns
     int blocks;  // summed by nuna_f8_matmul
+    int ytiles;  // of all groups, at most
     int xtiles;
     int items;   // workgroups that the tiles need at most
 };
@@ -153,21 +154,16 @@ __device__ __forceinline__ void band_order(uint32_t t, uint32_t ytiles, uint32_t
     yt = static_cast<int>(band * kBand + in - xt * h);
 }
 
-// The tile of work item `item`, or false.  Workgroup b runs on XCD b mod 8: each XCD takes a run of consecutive
-// tiles, so that a group's weights are read into one L2.
+// The tile of work item `item`, or false.  Each XCD takes a run of consecutive tiles, so that a group's weights are read
+// into one L2.
 template <int BY, bool WGRAD>
 __device__ __forceinline__ bool find_tile(const Shape& s, uint32_t item, Tile& tile) {
-    const uint32_t xcd = item & 7, seq = item >> 3;
-    const auto of_all = [&](uint32_t all, uint32_t& t) {
-        const uint32_t per = (all + 7) / 8;
-        t = xcd * per + seq;
-        return seq < per && t < all;
-    };
+    const uint32_t most = static_cast<uint32_t>(s.ytiles);
     uint32_t t;
     int yt;
     if constexpr (WGRAD) {
         const uint32_t ytiles = (s.ny + BY - 1) / BY, each = ytiles * s.xtiles;
-        if (!of_all(each * s.groups, t)) return false;
+        if (!xcd_tile(item, ytiles * s.groups, most, s.xtiles, t)) return false;
         tile.g = static_cast<int>(t / each);
         band_order(t - tile.g * each, ytiles, s.xtiles, yt, tile.xt);
         const int from = group_offset(s.offsets, tile.g, s.rows), to = group_offset(s.offsets, tile.g + 1, s.rows);
@@ -181,7 +177,7 @@ __device__ __forceinline__ bool find_tile(const Shape& s, uint32_t item, Tile& t
         tile.kb1 = s.blocks;
         if (!s.offsets) {
             const uint32_t ytiles = (s.ny + BY - 1) / BY;
-            if (!of_all(ytiles * s.xtiles, t)) return false;
+            if (!xcd_tile(item, ytiles, most, s.xtiles, t)) return false;
             band_order(t, ytiles, s.xtiles, yt, tile.xt);
             tile.g = 0;
             tile.y0 = yt * BY;
@@ -193,7 +189,9 @@ __device__ __forceinline__ bool find_tile(const Shape& s, uint32_t item, Tile& t
         uint32_t total = __builtin_amdgcn_readlane(upto, 63);
         for (int i = 64; i < s.groups; i += 64)
             total += __builtin_amdgcn_readlane(wave_inclusive(group_tiles<BY>(s.offsets, i + lane, s.groups, s.rows)), 63);
-        if (!of_all(total * s.xtiles, t)) return false;
+        // t and a group's tiles are below 2^31 each, so the search for t is exact even where a table that is not
+        // ascending makes a sum past it wrap.
+        if (!xcd_tile(item, total, most, s.xtiles, t)) return false;
         uint32_t before = 0;
         for (int i = 0; i < s.groups; i += 64) {
             if (i > 0) {
@@ -604,6 +602,7 @@ bool lay_out(Shape& shape) {
                                  : shape.offsets ? shape.ny / BY + std::min(shape.groups, shape.ny)
                                                  : (static_cast<int64_t>(shape.ny) + BY - 1) / BY;
     const int64_t items = (ytiles * xtiles + 7) / 8 * 8;
+    shape.ytiles = static_cast<int>(ytiles);
     shape.xtiles = static_cast<int>(xtiles);
     shape.items = static_cast<int>(items);
     return items <= INT32_MAX - (1 << 20);
@@ -660,7 +659,7 @@ hipError_t launch_f8_matmul(const void* a, const void* a_scale, const void* b, c
     const Operand Y = {static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(a_scale), k, scale_bytes};
     const Operand X = {static_cast<const uint8_t*>(b), static_cast<const uint8_t*>(b_scale), k, scale_bytes};
     const Shape shape = {offsets, groups, static_cast<int>(rows), static_cast<int>(rows), static_cast<int>(n),
-                         static_cast<int>(k / kF8Block), 0, 0};
+                         static_cast<int>(k / kF8Block), 0, 0, 0};
     // Which kernel, by the rows of a group (on average, with what the caller has room for) and the number of tiles.
     // Measured on MI355X, k = 7168 and n = 4096 where nothing else is said, us.  A larger tile moves less through the
     // L2 and LDS for each product, as long as there are tiles for the 256 compute units; tiles of few rows leave the
@@ -704,7 +703,7 @@ hipError_t launch_f8_wgrad(const void* a, const void* a_scale, const void* b, co
     const int64_t scale_bytes = f8_pitch(width) * static_cast<int64_t>(f8_scale_size(kind));
     const Operand Y = {static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(a_scale), width, scale_bytes};
     const Operand X = {static_cast<const uint8_t*>(b), static_cast<const uint8_t*>(b_scale), width, scale_bytes};
-    const Shape shape = {offsets, groups, static_cast<int>(rows), static_cast<int>(n), static_cast<int>(k), 0, 0, 0};
+    const Shape shape = {offsets, groups, static_cast<int>(rows), static_cast<int>(n), static_cast<int>(k), 0, 0, 0, 0};
     // Of groups of few rows the outputs are most of the work, and two smaller workgroups of a compute unit, of 8 waves
     // each, hide each other's stores: 32 groups of 256 rows, n = 2048, k = 7168, fp32 results, 587 us, with 4 waves of
     // 64 x 64 648, with 64 x 128 tiles 648, with 256 x 128 643.  (723 us where the operands' rows are a multiple of

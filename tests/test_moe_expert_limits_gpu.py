@@ -41,3 +41,27 @@ def test_columns_past_2_to_29_of_fp32_results(nuna):
     assert bool((out[0, 0] == b[:, 0].contiguous().view(F8).float()).all())
     del b, sb, out
     torch.cuda.empty_cache()
+
+
+def test_offsets_that_are_not_ascending_stay_in_the_buffers(nuna):
+    """A wrong table may give wrong results, but nothing outside the outputs is written; here the group whose rows no other
+    group names comes out right all the same."""
+    rows, n, k = 300, 200, 256
+    g = torch.Generator().manual_seed(1)
+    a, sa = nuna.f8_quantize(torch.randn((rows, k), generator=g).cuda())
+    b, sb = nuna.f8_quantize_blocks(torch.randn((6, n, k), generator=g).cuda())
+    off = torch.tensor([250, 300, 0, 120, 40, 200, -7], dtype=torch.int32, device="cuda")
+    whole = torch.full((rows * n + 512,), 7.0, device="cuda")
+    out = whole[256:-256].view(rows, n)
+    nuna.f8_matmul(a, sa, b, sb, out, offsets=off)
+    assert bool((whole[:256] == 7).all()) and bool((whole[-256:] == 7).all())
+    want = nuna.f8_matmul(a, sa, b[0], sb[0], out_dtype=torch.float32)
+    assert bool((out[250:] - want[250:]).abs().max() < 1e-3 * want.abs().max())
+    x = torch.randn((rows, 72), generator=g).cuda()
+    raw = torch.full((72 * ref.cols_width(rows, 6) + 512,), 0x3C, dtype=torch.uint8, device="cuda")
+    q = raw[256:-256].view(72, -1).view(F8)
+    qc, sc = nuna.f8_quantize_cols(x, off, "f32", q)
+    assert bool((raw[:256] == 0x3C).all()) and bool((raw[-256:] == 0x3C).all())
+    whole = torch.full((6 * 72 * 72 + 512,), 7.0, device="cuda")
+    nuna.f8_wgrad(qc, sc, qc, sc, off, whole[256:-256].view(6, 72, 72))
+    assert bool((whole[:256] == 7).all()) and bool((whole[-256:] == 7).all())
