@@ -19,7 +19,10 @@
  * algorithm and launch shape.  Copies (all-gather, all-to-all) move bytes.
  *
  * Placement (Sec. 4.2, Algorithm 1; configurations UA and NAP* of Sec. 5.3).
- * Workgroup b of a launch runs on XCD (b mod 8) on MI355X.
+ * Workgroup b of a launch runs on XCD (b + c) mod 8 on MI355X, c the same for
+ * all workgroups of a launch (0 in a process that has used one stream only;
+ * what follows relies on equal b mod 8 sharing an XCD, and calls it XCD b mod
+ * 8).
  *   NUNA_PLACE_LINEAR  work item w runs on workgroup w (grid-stride): the
  *                      round-robin, locality-unaware baseline (UA).
  *   NUNA_PLACE_XCD     work items that touch the same data form one logical
@@ -127,8 +130,9 @@ typedef enum {
  * topology to the placement step; this is where the library learns it).
  * Checks that the device is gfx950, then launches 2048 one-wave workgroups
  * that each record the XCC they ran on, and verifies the dispatch map XCD
- * placement relies on: 256 compute units and workgroup b on XCD b mod 8 for
- * every b (nuna_check_dispatch_map).  Allocates 8 KiB of device memory for
+ * placement relies on: 256 compute units and workgroup b on XCD (b + c) mod 8
+ * for every b, c being workgroup 0's XCD (nuna_check_dispatch_map on the XCCs
+ * counted from there), so it may be called after work on other streams.  Allocates 8 KiB of device memory for
  * the probe and frees it; synchronous, not capturable.  Idempotent and
  * thread-safe; call it once on every device before XCD-mode collectives
  * (LINEAR-mode calls work without it).  Returns NUNA_ERR_HIP without a
@@ -141,7 +145,7 @@ typedef struct {
     int32_t device;       /* HIP device ordinal */
     int32_t cu_count;     /* compute units */
     int32_t xcd_count;    /* distinct XCC ids seen by the probe (1 + largest) */
-    int32_t map_verified; /* 1: workgroup b runs on XCD b mod 8; XCD placement available */
+    int32_t map_verified; /* 1: workgroup b runs on XCD (b + c) mod 8; XCD placement available */
 } nuna_device_info_t;
 
 /* Fill *info for the current device.  NUNA_ERR_INVALID_ARG if nuna_init has
@@ -172,7 +176,7 @@ typedef struct {
 nuna_status_t nuna_last_launch(nuna_launch_info_t* info);
 
 /* Host-only check behind nuna_init (no HIP call): xcc[b] is the XCC
- * workgroup b of a G-workgroup launch ran on (HOST int32 array, G >= 64).
+ * workgroup b of a G-workgroup launch ran on, counted from workgroup 0's (HOST int32 array, G >= 64).
  * NUNA_OK if cu_count is 256 and xcc[b] == b mod 8 for every b, else
  * NUNA_ERR_UNSUPPORTED naming the first mismatch (NUNA_ERR_INVALID_ARG for a
  * NULL array or G < 64). */

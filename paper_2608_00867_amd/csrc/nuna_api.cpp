@@ -289,8 +289,8 @@ std::atomic<void*> g_scratch[kMaxDevices];
 // Workgroups the init probe launches: a few per compute unit, in many rounds of 8.
 constexpr int kProbeGrid = 2048;
 
-// XCD placement relies on the hardware running workgroup b on XCD b mod 8
-// (placement.h).  Before the first XCD-mode call on a device, nuna_init must
+// XCD placement relies on the hardware running workgroup b on XCD (b + c) mod
+// 8 (placement.h).  Before the first XCD-mode call on a device, nuna_init must
 // have verified that map there; a device where it does not hold (another
 // partition mode, another chip) gets NUNA_ERR_UNSUPPORTED for XCD mode rather
 // than a placement the kernels do not intend.  LINEAR needs no map.
@@ -304,7 +304,7 @@ nuna_status_t check_placement_ready(int place) {
     if (st == kMapFailed)
         return fail(NUNA_ERR_UNSUPPORTED,
                     "XCD placement is unavailable on device %d: nuna_init found that workgroup b does not run on "
-                    "XCD b mod %d there",
+                    "XCD (b + c) mod %d there",
                     dev, NUNA_NUM_XCD);
     return fail(NUNA_ERR_UNSUPPORTED,
                 "XCD placement needs nuna_init() on device %d first (it verifies the workgroup -> XCD dispatch map)",
@@ -393,6 +393,13 @@ nuna_status_t nuna_init(void) try {
     if ((e = nuna::routed_scratch_address(&scr)) != hipSuccess || !scr)
         return hip_status(e != hipSuccess ? e : hipErrorInvalidSymbol, "hipGetSymbolAddress (scratch)");
     g_scratch[dev].store(scr, std::memory_order_release);
+    // Once a process has captured a graph or used several streams, workgroup 0 may run on another XCD (observed: 7,
+    // then 6).  Groups stay together all the same, so the map is checked relative to workgroup 0.  (Ids outside
+    // [0, 8) are left as they are, for the check to refuse.)
+    if (std::all_of(xcc.begin(), xcc.end(), [](int32_t x) { return x >= 0 && x < NUNA_NUM_XCD; })) {
+        const int32_t first = xcc[0];
+        for (int32_t& x : xcc) x = (x - first + NUNA_NUM_XCD) % NUNA_NUM_XCD;
+    }
     const nuna_status_t st = nuna_check_dispatch_map(xcc.data(), kProbeGrid, prop.multiProcessorCount);
     g_map_state[dev].store(st == NUNA_OK ? kMapVerified : kMapFailed, std::memory_order_release);
     if (st != NUNA_OK) {

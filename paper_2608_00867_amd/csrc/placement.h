@@ -9,7 +9,9 @@
 // Algorithm 1 places each group as a unit).  Groups may also have variable
 // sizes (all-to-all); the host then lists the items in placement order.
 //
-// MI355X dispatches workgroup b of a launch to XCD (b mod 8).  With G
+// MI355X dispatches workgroup b of a launch to XCD (b mod 8), or, in a process
+// that has used several streams, to that XCD turned by the same number for
+// all workgroups; only that equal b mod 8 share an XCD matters here.  With G
 // workgroups, XCD x holds Gx = ceil((G - x) / 8) of them; its k-th one has
 // k = b div 8.
 //
