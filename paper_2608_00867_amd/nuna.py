@@ -587,6 +587,8 @@ def all_to_all_combine(y, out, layout, placement="xcd", stream=None, weights=Non
 
 
 # ------------------------------------------------------------------ the expert layer
+#
+# All tensors of a call are on the current device, and so is the stream.
 
 SCALES = {"f32": SCALE_F32, "e8m0": SCALE_E8M0}
 
@@ -622,25 +624,43 @@ def _scale_dtype(scale):
     return torch.float32 if scale == "f32" else torch.float8_e8m0fnu
 
 
-def _handle(stream, t):
-    """The stream to enqueue on: that given (a torch stream or a raw handle), or torch's current one of t's device.
+def _current_device():
+    return _torch()._C._cuda_getDevice()
+
+
+def _device_of(t, name):
+    """The device of a call's first tensor, which has to be the current one: kernels are launched there."""
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a CUDA tensor, got {list(t.shape)} of {t.dtype} on the CPU")
+    if dev != _current_device():
+        raise ValueError(f"{name} is on device {dev}, the current one is {_current_device()}")
+    return dev
+
+
+def _handle(stream, dev):
+    """The stream to enqueue on: that given (a torch stream or a raw handle), or torch's current one of device `dev`.
     The raw handle is asked for directly: making the Stream object took 2.7 us, of calls of 4 to 5 us."""
     if stream is None:
-        return _torch()._C._cuda_getCurrentRawStream(t.get_device())
-    return stream if isinstance(stream, int) else stream.cuda_stream
+        return _torch()._C._cuda_getCurrentRawStream(dev)
+    if isinstance(stream, int):
+        return stream
+    if stream.device_index != dev:
+        raise ValueError(f"a stream of device {stream.device_index} for tensors on device {dev}")
+    return stream.cuda_stream
 
 
-def _check_tensor(t, name, shape, dtype):
-    """A contiguous CUDA tensor of this shape (a tuple) and dtype."""
-    if not (t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous CUDA tensor {list(shape)} of {dtype}, "
-                         f"got {list(t.shape)} of {t.dtype}")
+def _check_tensor(t, name, shape, dtype, dev):
+    """A contiguous tensor of this shape (a tuple) and dtype on device `dev`."""
+    if not (t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous CUDA tensor {list(shape)} of {dtype} on device {dev}, "
+                         f"got {list(t.shape)} of {t.dtype} on {t.device}")
 
 
-def _check_matrix(t, name):
-    """A CUDA tensor [rows, cols] whose rows are contiguous; returns its row stride."""
-    if not t.is_cuda or t.dim() != 2:
-        raise ValueError(f"{name} must be a CUDA tensor [rows, cols] with contiguous rows")
+def _check_matrix(t, name, dev):
+    """A tensor [rows, cols] on device `dev` whose rows are contiguous; returns its row stride."""
+    if t.get_device() != dev or t.dim() != 2:
+        raise ValueError(f"{name} must be a CUDA tensor [rows, cols] with contiguous rows, on device {dev}")
     rows, cols = t.shape
     if t.is_contiguous() and cols:
         return cols
@@ -652,15 +672,15 @@ def _check_matrix(t, name):
     return stride
 
 
-def _check_table(t, name):
-    if not (t.is_cuda and t.dtype is _torch().int32 and t.dim() == 2 and t.is_contiguous() and t.shape[1]):
-        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor [tokens, topk]")
+def _check_table(t, name, dev):
+    if not (t.get_device() == dev and t.dtype is _torch().int32 and t.dim() == 2 and t.is_contiguous() and t.shape[1]):
+        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor [tokens, topk], on device {dev}")
     return t.shape
 
 
-def _check_offsets(t):
-    if not t.is_cuda or not t.is_contiguous() or t.dim() != 1 or t.dtype != _torch().int32 or t.numel() < 2:
-        raise ValueError("offsets must be a contiguous int32 CUDA tensor [groups + 1]")
+def _check_offsets(t, dev):
+    if t.get_device() != dev or not t.is_contiguous() or t.dim() != 1 or t.dtype != _torch().int32 or t.numel() < 2:
+        raise ValueError(f"offsets must be a contiguous int32 CUDA tensor [groups + 1], on device {dev}")
     return t.numel() - 1
 
 
@@ -675,15 +695,15 @@ def _new(stream, shape, dtype, device):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _f8_outputs(out, scale_out, shape, scale_shape, scale, stream, device):
+def _f8_outputs(out, scale_out, shape, scale_shape, scale, stream, device, dev):
     """The 8-bit output and its scales: those given, checked, or new ones of the scale type `scale`."""
     torch = _torch()
     if out is None:
         out = _new(stream, shape, torch.float8_e4m3fn, device)
     if scale_out is None:
         scale_out = _new(stream, scale_shape, _scale_dtype(scale), device)
-    _check_tensor(out, "out", shape, torch.float8_e4m3fn)
-    _check_tensor(scale_out, "scale_out", scale_shape, _scale_dtype(scale))
+    _check_tensor(out, "out", shape, torch.float8_e4m3fn, dev)
+    _check_tensor(scale_out, "scale_out", scale_shape, _scale_dtype(scale), dev)
     return out, scale_out
 
 
@@ -703,7 +723,8 @@ def moe_sort(topk_idx, num_experts, first_expert=0, offsets=None, slot_of=None, 
     last), row_of[t, j] a slot's row (-1: none).  Where none of them is given they are parts of one allocation.
     workspace: a uint8 CUDA tensor of moe_sort_workspace bytes."""
     torch = _torch()
-    T, k = _check_table(topk_idx, "topk_idx")
+    index = _device_of(topk_idx, "topk_idx")
+    T, k = _check_table(topk_idx, "topk_idx", index)
     num_experts = int(num_experts)
     need = moe_sort_workspace(T, k, num_experts)
     dev, n = topk_idx.device, T * k
@@ -721,16 +742,16 @@ def moe_sort(topk_idx, num_experts, first_expert=0, offsets=None, slot_of=None, 
         offsets = _new(stream, (num_experts + 1,), torch.int32, dev) if offsets is None else offsets
         slot_of = _new(stream, (n,), torch.int32, dev) if slot_of is None else slot_of
         row_of = _new(stream, (T, k), torch.int32, dev) if row_of is None else row_of
-        _check_tensor(offsets, "offsets", (num_experts + 1,), torch.int32)
-        _check_tensor(slot_of, "slot_of", (n,), torch.int32)
-        _check_tensor(row_of, "row_of", (T, k), torch.int32)
+        _check_tensor(offsets, "offsets", (num_experts + 1,), torch.int32, index)
+        _check_tensor(slot_of, "slot_of", (n,), torch.int32, index)
+        _check_tensor(row_of, "row_of", (T, k), torch.int32, index)
     if workspace is None:
         workspace = _new(stream, (need,), torch.uint8, dev) if need else None
-    elif not workspace.is_cuda or not workspace.is_contiguous() or workspace.dtype != torch.uint8:
-        raise ValueError("workspace must be a contiguous uint8 CUDA tensor")
+    elif workspace.get_device() != index or not workspace.is_contiguous() or workspace.dtype != torch.uint8:
+        raise ValueError(f"workspace must be a contiguous uint8 CUDA tensor on device {index}")
     _check(lib().nuna_moe_sort(topk_idx.data_ptr(), T, k, int(first_expert), num_experts, offsets.data_ptr(),
                                slot_of.data_ptr(), row_of.data_ptr(), workspace.data_ptr() if need else None,
-                               workspace.numel() if need else 0, _handle(stream, topk_idx)))
+                               workspace.numel() if need else 0, _handle(stream, index)))
     return offsets, slot_of, row_of
 
 
@@ -740,8 +761,9 @@ def moe_gather(x, row_of, out, scale_out=None, stream=None):
     f8_pitch(H)] (float32 or float8_e8m0fnu): each row quantised as f8_quantize does.  Returns out, or (out,
     scale_out).  The gradient of the first form is moe_scatter without weights."""
     torch = _torch()
-    T, k = _check_table(row_of, "row_of")
-    stride = _check_matrix(x, "x")
+    dev = _device_of(x, "x")
+    T, k = _check_table(row_of, "row_of", dev)
+    stride = _check_matrix(x, "x", dev)
     H = x.shape[1]
     if x.shape[0] != T:
         raise ValueError(f"x has {x.shape[0]} rows, row_of {T}")
@@ -749,37 +771,38 @@ def moe_gather(x, row_of, out, scale_out=None, stream=None):
         raise ValueError("out must be [rows, columns]")
     cap = out.shape[0]
     if scale_out is None:
-        _check_tensor(out, "out", (cap, H), x.dtype)
+        _check_tensor(out, "out", (cap, H), x.dtype, dev)
         _check(lib().nuna_moe_gather(x.data_ptr(), stride, row_of.data_ptr(), T, k, H, out.data_ptr(), cap,
-                                     _dtype_code(x), _handle(stream, x)))
+                                     _dtype_code(x), _handle(stream, dev)))
         return out
-    _check_tensor(out, "out", (cap, f8_width(H)), torch.float8_e4m3fn)
+    _check_tensor(out, "out", (cap, f8_width(H)), torch.float8_e4m3fn, dev)
     kind = _scale_kind(scale_out, "scale_out")
-    _check_tensor(scale_out, "scale_out", (cap, f8_pitch(H)), scale_out.dtype)
+    _check_tensor(scale_out, "scale_out", (cap, f8_pitch(H)), scale_out.dtype, dev)
     _check(lib().nuna_moe_gather_f8(x.data_ptr(), stride, row_of.data_ptr(), T, k, H, out.data_ptr(),
-                                    scale_out.data_ptr(), cap, _dtype_code(x), kind, _handle(stream, x)))
+                                    scale_out.data_ptr(), cap, _dtype_code(x), kind, _handle(stream, dev)))
     return out, scale_out
 
 
-def _check_weights(weights, T, k):
-    _check_tensor(weights, "weights", (T, k), _torch().float32)
+def _check_weights(weights, T, k, dev):
+    _check_tensor(weights, "weights", (T, k), _torch().float32, dev)
     return weights.data_ptr()
 
 
 def moe_scatter(y, row_of, weights=None, out=None, stream=None):
     """out[t] = sum over j, ascending, of weights[t, j] * y[row_of[t, j]] (float32 weights [T, k], or None: 1) over
     the slots with a row of y; fp32 sums, rounded once.  A token without a row gets zeros."""
-    T, k = _check_table(row_of, "row_of")
+    dev = _device_of(y, "y")
+    T, k = _check_table(row_of, "row_of", dev)
     if y.dim() != 2:
         raise ValueError("y must be [rows, columns]")
     cap, H = y.shape
-    _check_tensor(y, "y", (cap, H), y.dtype)
-    wp = None if weights is None else _check_weights(weights, T, k)
+    _check_tensor(y, "y", (cap, H), y.dtype, dev)
+    wp = None if weights is None else _check_weights(weights, T, k, dev)
     if out is None:
         out = _new(stream, (T, H), y.dtype, y.device)
-    _check_tensor(out, "out", (T, H), y.dtype)
+    _check_tensor(out, "out", (T, H), y.dtype, dev)
     _check(lib().nuna_moe_scatter(y.data_ptr(), row_of.data_ptr(), wp, T, k, H, cap, out.data_ptr(), _dtype_code(y),
-                                  _handle(stream, y)))
+                                  _handle(stream, dev)))
     return out
 
 
@@ -788,51 +811,54 @@ def moe_scatter_grad(dout, y, row_of, weights, dy=None, dweights=None, stream=No
     <dout[t], y[row_of[t, j]]> (fp32; 0 for a slot without a row).  Rows of dy that no slot names are left untouched,
     and are zeros where dy is not given."""
     torch = _torch()
-    T, k = _check_table(row_of, "row_of")
+    dev = _device_of(y, "y")
+    T, k = _check_table(row_of, "row_of", dev)
     if y.dim() != 2:
         raise ValueError("y must be [rows, columns]")
     cap, H = y.shape
-    _check_tensor(y, "y", (cap, H), y.dtype)
-    _check_tensor(dout, "dout", (T, H), y.dtype)
-    wp = _check_weights(weights, T, k)
+    _check_tensor(y, "y", (cap, H), y.dtype, dev)
+    _check_tensor(dout, "dout", (T, H), y.dtype, dev)
+    wp = _check_weights(weights, T, k, dev)
     if dy is None:
         dy = _new(stream, (cap, H), y.dtype, y.device)
         with torch.cuda.stream(stream):
             dy.zero_()
     if dweights is None:
         dweights = _new(stream, (T, k), torch.float32, y.device)
-    _check_tensor(dy, "dy", (cap, H), y.dtype)
-    _check_tensor(dweights, "dweights", (T, k), torch.float32)
+    _check_tensor(dy, "dy", (cap, H), y.dtype, dev)
+    _check_tensor(dweights, "dweights", (T, k), torch.float32, dev)
     _check(lib().nuna_moe_scatter_grad(dout.data_ptr(), y.data_ptr(), row_of.data_ptr(), wp, T, k, H, cap,
-                                       dy.data_ptr(), dweights.data_ptr(), _dtype_code(y), _handle(stream, y)))
+                                       dy.data_ptr(), dweights.data_ptr(), _dtype_code(y), _handle(stream, dev)))
     return dy, dweights
 
 
 def f8_quantize(x, scale="f32", out=None, scale_out=None, stream=None):
     """x [rows, cols] (contiguous rows) to e4m3 with a scale ("f32" or "e8m0") for every 128 columns of a row.  Returns
     (out float8_e4m3fn [rows, f8_width(cols)], zeros past the last column; scale_out [rows, f8_pitch(cols)])."""
-    stride = _check_matrix(x, "x")
+    dev = _device_of(x, "x")
+    stride = _check_matrix(x, "x", dev)
     rows, cols = x.shape
     out, scale_out = _f8_outputs(out, scale_out, (rows, f8_width(cols)), (rows, f8_pitch(cols)), scale, stream,
-                                 x.device)
+                                 x.device, dev)
     _check(lib().nuna_f8_quantize(x.data_ptr(), stride, rows, cols, _dtype_code(x), out.data_ptr(),
-                                  scale_out.data_ptr(), SCALES[scale], _handle(stream, x)))
+                                  scale_out.data_ptr(), SCALES[scale], _handle(stream, dev)))
     return out, scale_out
 
 
 def f8_quantize_blocks(x, scale="f32", out=None, scale_out=None, stream=None):
     """Weights x [.., rows, cols] to e4m3 with a scale for every block of 128 x 128.  Returns (out [.., rows,
     f8_width(cols)], scale_out [.., ceil(rows / 128), f8_pitch(cols)])."""
-    if not x.is_cuda or not x.is_contiguous() or x.dim() < 2 or x.shape[-1] < 1:
+    dev = _device_of(x, "x")
+    if not x.is_contiguous() or x.dim() < 2 or x.shape[-1] < 1:
         raise ValueError("x must be a contiguous CUDA tensor [.., rows, cols]")
     lead, (rows, cols) = tuple(x.shape[:-2]), x.shape[-2:]
     batch = 1
     for n in lead:
         batch *= n
     out, scale_out = _f8_outputs(out, scale_out, (*lead, rows, f8_width(cols)),
-                                 (*lead, -(-rows // F8_BLOCK), f8_pitch(cols)), scale, stream, x.device)
+                                 (*lead, -(-rows // F8_BLOCK), f8_pitch(cols)), scale, stream, x.device, dev)
     _check(lib().nuna_f8_quantize_blocks(x.data_ptr(), batch, rows, cols, _dtype_code(x), out.data_ptr(),
-                                         scale_out.data_ptr(), SCALES[scale], _handle(stream, x)))
+                                         scale_out.data_ptr(), SCALES[scale], _handle(stream, dev)))
     return out, scale_out
 
 
@@ -842,18 +868,20 @@ def f8_quantize_cols(x, offsets, scale="f32", out=None, scale_out=None, slot_of=
     x, so that x need not be gathered first.  Returns (out [cols, f8_cols_width(rows, groups)], scale_out), the
     operands of f8_wgrad."""
     torch = _torch()
-    stride = _check_matrix(x, "x")
-    groups = _check_offsets(offsets)
+    dev = _device_of(x, "x")
+    stride = _check_matrix(x, "x", dev)
+    groups = _check_offsets(offsets, dev)
     x_rows, cols = x.shape
     rows = x_rows
     if slot_of is not None:
         rows = slot_of.numel()
-        _check_tensor(slot_of, "slot_of", (rows,), torch.int32)
+        _check_tensor(slot_of, "slot_of", (rows,), torch.int32, dev)
     width = f8_cols_width(rows, groups)
-    out, scale_out = _f8_outputs(out, scale_out, (cols, width), (cols, f8_pitch(width)), scale, stream, x.device)
+    out, scale_out = _f8_outputs(out, scale_out, (cols, width), (cols, f8_pitch(width)), scale, stream, x.device,
+                                 dev)
     _check(lib().nuna_f8_quantize_cols(x.data_ptr(), stride, x_rows, None if slot_of is None else slot_of.data_ptr(),
                                        int(topk), offsets.data_ptr(), groups, rows, cols, _dtype_code(x),
-                                       out.data_ptr(), scale_out.data_ptr(), SCALES[scale], _handle(stream, x)))
+                                       out.data_ptr(), scale_out.data_ptr(), SCALES[scale], _handle(stream, dev)))
     return out, scale_out
 
 
@@ -864,22 +892,23 @@ def f8_matmul(a, a_scale, b, b_scale, out=None, offsets=None, out_dtype=None, st
     untouched."""
     torch = _torch()
     f8 = torch.float8_e4m3fn
-    groups = 1 if offsets is None else _check_offsets(offsets)
+    dev = _device_of(a, "a")
+    groups = 1 if offsets is None else _check_offsets(offsets, dev)
     lead = () if offsets is None else (groups,)
     if a.dim() != 2 or b.dim() != 2 + len(lead):
         raise ValueError("a must be [rows, k] and b [n, k], or [groups, n, k] with offsets")
     (rows, k), n = a.shape, b.shape[-2]
     kind = _scale_kind(a_scale, "a_scale")
-    _check_tensor(a, "a", (rows, k), f8)
-    _check_tensor(b, "b", (*lead, n, k), f8)
-    _check_tensor(a_scale, "a_scale", (rows, f8_pitch(k)), a_scale.dtype)
-    _check_tensor(b_scale, "b_scale", (*lead, -(-n // F8_BLOCK), f8_pitch(k)), a_scale.dtype)
+    _check_tensor(a, "a", (rows, k), f8, dev)
+    _check_tensor(b, "b", (*lead, n, k), f8, dev)
+    _check_tensor(a_scale, "a_scale", (rows, f8_pitch(k)), a_scale.dtype, dev)
+    _check_tensor(b_scale, "b_scale", (*lead, -(-n // F8_BLOCK), f8_pitch(k)), a_scale.dtype, dev)
     if out is None:
         out = _new(stream, (rows, n), out_dtype or torch.bfloat16, a.device)
-    _check_tensor(out, "out", (rows, n), out_dtype or out.dtype)
+    _check_tensor(out, "out", (rows, n), out_dtype or out.dtype, dev)
     _check(lib().nuna_f8_matmul(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),
                                 None if offsets is None else offsets.data_ptr(), groups, rows, n, k, out.data_ptr(),
-                                kind, _dtype_code(out), _handle(stream, a)))
+                                kind, _dtype_code(out), _handle(stream, dev)))
     return out
 
 
@@ -889,7 +918,8 @@ def f8_wgrad(a, a_scale, b, b_scale, offsets, out=None, out_dtype=None, stream=N
     (float32 unless given), zeros for a group without rows."""
     torch = _torch()
     f8 = torch.float8_e4m3fn
-    groups = _check_offsets(offsets)
+    dev = _device_of(a, "a")
+    groups = _check_offsets(offsets, dev)
     if a.dim() != 2 or b.dim() != 2:
         raise ValueError("a must be [n, width] and b [k, width]")
     (n, width), k = a.shape, b.shape[0]
@@ -897,15 +927,15 @@ def f8_wgrad(a, a_scale, b, b_scale, offsets, out=None, out_dtype=None, stream=N
     if width % F8_BLOCK or rows < 0:
         raise ValueError(f"a of {width} columns is no layout of {groups} groups")
     kind = _scale_kind(a_scale, "a_scale")
-    _check_tensor(a, "a", (n, width), f8)
-    _check_tensor(b, "b", (k, width), f8)
-    _check_tensor(a_scale, "a_scale", (n, f8_pitch(width)), a_scale.dtype)
-    _check_tensor(b_scale, "b_scale", (k, f8_pitch(width)), a_scale.dtype)
+    _check_tensor(a, "a", (n, width), f8, dev)
+    _check_tensor(b, "b", (k, width), f8, dev)
+    _check_tensor(a_scale, "a_scale", (n, f8_pitch(width)), a_scale.dtype, dev)
+    _check_tensor(b_scale, "b_scale", (k, f8_pitch(width)), a_scale.dtype, dev)
     if out is None:
         out = _new(stream, (groups, n, k), out_dtype or torch.float32, a.device)
-    _check_tensor(out, "out", (groups, n, k), out_dtype or out.dtype)
+    _check_tensor(out, "out", (groups, n, k), out_dtype or out.dtype, dev)
     _check(lib().nuna_f8_wgrad(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), offsets.data_ptr(),
-                               groups, rows, n, k, out.data_ptr(), kind, _dtype_code(out), _handle(stream, a)))
+                               groups, rows, n, k, out.data_ptr(), kind, _dtype_code(out), _handle(stream, dev)))
     return out
 
 
