@@ -889,7 +889,7 @@ def f8_matmul(a, a_scale, b, b_scale, out=None, offsets=None, out_dtype=None, st
     """out[r] = b[g] @ a[r] in 8 bits, g the group of row r.  a [rows, k] with its scales (f8_quantize), b [groups, n,
     k] with its block scales (f8_quantize_blocks); offsets int32 [groups + 1] (moe_sort); without offsets b is [n, k]
     and every row is multiplied by it.  out [rows, n] of out_dtype (bfloat16 unless given); rows in no group are left
-    untouched."""
+    untouched, and are zeros where out is not given."""
     torch = _torch()
     f8 = torch.float8_e4m3fn
     dev = _device_of(a, "a")
@@ -905,6 +905,9 @@ def f8_matmul(a, a_scale, b, b_scale, out=None, offsets=None, out_dtype=None, st
     _check_tensor(b_scale, "b_scale", (*lead, -(-n // F8_BLOCK), f8_pitch(k)), a_scale.dtype, dev)
     if out is None:
         out = _new(stream, (rows, n), out_dtype or torch.bfloat16, a.device)
+        if offsets is not None:
+            with torch.cuda.stream(stream):
+                out.zero_()
     _check_tensor(out, "out", (rows, n), out_dtype or out.dtype, dev)
     _check(lib().nuna_f8_matmul(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),
                                 None if offsets is None else offsets.data_ptr(), groups, rows, n, k, out.data_ptr(),

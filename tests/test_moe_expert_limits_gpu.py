@@ -65,3 +65,22 @@ def test_offsets_that_are_not_ascending_stay_in_the_buffers(nuna):
     whole = torch.full((6 * 72 * 72 + 512,), 7.0, device="cuda")
     nuna.f8_wgrad(qc, sc, qc, sc, off, whole[256:-256].view(6, 72, 72))
     assert bool((whole[:256] == 7).all()) and bool((whole[-256:] == 7).all())
+
+
+def test_product_without_out_leaves_no_old_memory(nuna):
+    """Rows that no group holds are zeros where the call makes the output itself, as moe_scatter_grad's are."""
+    rows, n, k = 512, 1024, 256
+    a, sa = nuna.f8_quantize(torch.randn((rows, k), device="cuda"))
+    b, sb = nuna.f8_quantize_blocks(torch.randn((3, n, k), device="cuda"))
+    off = torch.tensor([5, 100, 100, 300], dtype=torch.int32, device="cuda")
+    for dtype in (torch.bfloat16, torch.float32):
+        for stream in (None, torch.cuda.Stream()):
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                old = torch.full((rows, n), float("nan"), dtype=dtype, device="cuda")
+            torch.cuda.synchronize()
+            del old
+            out = nuna.f8_matmul(a, sa, b, sb, offsets=off, out_dtype=dtype, stream=stream)
+            torch.cuda.synchronize()
+            assert bool((out[:5] == 0).all()) and bool((out[300:] == 0).all()) and bool(out.isfinite().all())
+            assert bool((out[5:300] != 0).any(1).all())
