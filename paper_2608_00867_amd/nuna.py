@@ -889,7 +889,8 @@ def f8_matmul(a, a_scale, b, b_scale, out=None, offsets=None, out_dtype=None, st
     """out[r] = b[g] @ a[r] in 8 bits, g the group of row r.  a [rows, k] with its scales (f8_quantize), b [groups, n,
     k] with its block scales (f8_quantize_blocks); offsets int32 [groups + 1] (moe_sort); without offsets b is [n, k]
     and every row is multiplied by it.  out [rows, n] of out_dtype (bfloat16 unless given); rows in no group are left
-    untouched, and are zeros where out is not given."""
+    untouched, and are zeros where out is not given.  fp32 results come from exact products and fp32 sums; for bfloat16
+    the 8-bit matrix instructions lose up to 7 * 2^-13 of the largest product of every 8 (include/nuna.h)."""
     torch = _torch()
     f8 = torch.float8_e4m3fn
     dev = _device_of(a, "a")
@@ -918,7 +919,7 @@ def f8_matmul(a, a_scale, b, b_scale, out=None, offsets=None, out_dtype=None, st
 def f8_wgrad(a, a_scale, b, b_scale, offsets, out=None, out_dtype=None, stream=None):
     """Gradient of grouped weights: out[g] = sum over the rows r of group g of a[:, r] b[:, r]^T.  a [n, width] and
     b [k, width] with their scales, both of f8_quantize_cols with these offsets.  out [groups, n, k] of out_dtype
-    (float32 unless given), zeros for a group without rows."""
+    (float32 unless given; it chooses the sums' precision as in f8_matmul), zeros for a group without rows."""
     torch = _torch()
     f8 = torch.float8_e4m3fn
     dev = _device_of(a, "a")

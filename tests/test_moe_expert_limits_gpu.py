@@ -84,3 +84,120 @@ def test_product_without_out_leaves_no_old_memory(nuna):
             torch.cuda.synchronize()
             assert bool((out[:5] == 0).all()) and bool((out[300:] == 0).all()) and bool(out.isfinite().all())
             assert bool((out[5:300] != 0).any(1).all())
+
+
+# ------------------------------------------------------------------ helpers
+
+def cut_rows(rows, groups, seed):
+    """Offsets of `groups` groups of uneven sizes, some of them empty."""
+    cuts = np.sort(np.random.default_rng(seed).integers(0, rows + 1, groups - 1))
+    return np.concatenate([[0], cuts, [rows]]).astype(np.int32)
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def host(t):
+    t = t.detach().cpu()
+    if t.dtype == E8M0:
+        e = t.view(torch.uint8).numpy().astype(np.float64)
+        return np.where(e == 255, np.nan, 2.0 ** (e - 127))
+    if t.dtype == F8:
+        return ref.E4M3[t.view(torch.uint8).numpy()]
+    return t.double().numpy()
+
+
+def values8(q, s, row_block=1):
+    """Float64 values of an 8-bit matrix [n, k]."""
+    blocks = q.shape[1] // 128
+    return ref.dequantize(host(q), host(s)[:, :blocks], row_block)
+
+
+def normal(shape, seed):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed))
+
+
+EPS = 2.0 ** -24
+RUN = 8  # consecutive values whose products the 8-bit instructions cut together
+
+
+def sum_bound(a, b, k):
+    """(k + 4) additions in fp32, each off by at most a unit in the last place, of a [r, k] by b [c, k]."""
+    return 2 * (k + 4) * EPS * (np.abs(a) @ np.abs(b).T)
+
+
+def cut_bound(a, b):
+    """What the 8-bit instructions may lose besides: in every run of eight consecutive products, each of the seven others
+    less than 2^-13 of the power of two at or below the largest."""
+    p = np.abs(a[:, None, :] * b[None]).reshape(a.shape[0], b.shape[0], -1, RUN)
+    return 7 * 2.0 ** -13 * p.max(3).sum(2)
+
+
+def bounded(got, want, bound, what=""):
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} out of bounds, first at {np.argwhere(bad)[0]}: " \
+        f"{got[bad][0]} for {want[bad][0]}, bound {np.broadcast_to(bound, got.shape)[bad][0]}"
+
+
+# ------------------------------------------------------------------ what the sums hold
+
+def outliers(rows, k, seed):
+    """Rows with a few channels some 2^13 times the others, which cancel against weights of 1: what is left is the sum
+    of the small ones, and a small one beside an outlier is the first thing that a sum of few bits loses."""
+    g = np.random.default_rng(seed)
+    a = g.choice([1, 1.125, 1.25, 1.5, 1.75, 1.875], (rows, k)) * 2.0 ** g.integers(-6, -4, (rows, 1))
+    for r in range(rows):
+        for block in range(0, k, 128):
+            at = block + g.choice(128, 6, replace=False)
+            a[r, at[:3]], a[r, at[3:]] = 256, -256
+    return a
+
+
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+@pytest.mark.parametrize("rows,n,k,kernel", [(3, 24, 128, "k_f8_few"), (20, 300, 512, "k_f8_few"),
+                                             (300, 2101, 256, "k_f8_tiles"), (1000, 6201, 128, "k_f8_tiles")])
+def test_blocks_with_outliers(nuna, rows, n, k, kernel, kind, out):
+    """The values are held exactly in 8 bits with a scale of 1, so the error is the sum's alone.  Results in fp32 are held
+    to fp32 sums, less than a tenth of what the 8-bit instructions may cut."""
+    a = np.tile(outliers(min(rows, 40), k, rows), (-(-rows // 40), 1))[:rows]
+    b = np.tile(2.0 ** np.arange(-1, 2)[:, None], (-(-n // 3), k))[:n]
+    q = [torch.from_numpy(t).float().cuda().to(F8) for t in (a, b)]
+    assert all(np.array_equal(host(t), w) for t, w in zip(q, (a, b)))
+
+    def ones(r):
+        s = torch.ones((r, ref.pitch(k)), device="cuda")
+        return s if kind == "f32" else torch.full(s.shape, 127, dtype=torch.uint8, device="cuda").view(E8M0)
+
+    got = host(nuna.f8_matmul(q[0], ones(rows), q[1], ones(-(-n // 128)), out_dtype=out))
+    assert nuna.last_launch()["kernels"] == kernel
+    few, cols = min(rows, 40), min(n, 3)  # the rest repeats these
+    want, bound = a[:few] @ b[:cols].T, sum_bound(a[:few], b[:cols], k)
+    if out == torch.bfloat16:
+        cut = cut_bound(a[:few], b[:cols])
+        assert (cut > 10 * bound).all()
+        bound = bound + cut + 2.0 ** -8 * np.abs(want)
+    spread = [np.tile(t, (-(-rows // few), -(-n // cols)))[:rows, :n] for t in (want, bound)]
+    bounded(got, *spread)
+
+
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+@pytest.mark.parametrize("rows,n", [(2, 24), (300, 2101)])
+def test_small_blocks_after_a_large_one(nuna, rows, n, kind, out):
+    """The sum over the blocks is held in fp32: sums of 2^-19 of it and less are not lost from block to block."""
+    k = 128 * 12
+    a = np.zeros((rows, k))
+    a[:, :128] = 256
+    a[:, 128:-128:4] = 2.0 ** -4 * (1 + np.arange(rows)[:, None] % 3)
+    a[:, -128:] = -256
+    q = torch.from_numpy(a).float().cuda().to(F8), torch.ones((n, k), device="cuda").to(F8)
+
+    def ones(r):
+        s = torch.ones((r, ref.pitch(k)), device="cuda")
+        return s if kind == "f32" else torch.full(s.shape, 127, dtype=torch.uint8, device="cuda").view(E8M0)
+
+    got = host(nuna.f8_matmul(q[0], ones(rows), q[1], ones(-(-n // 128)), out_dtype=out))
+    want = np.tile(a.sum(1)[:, None], (1, n))  # of numbers that fp32 holds exactly, bf16 with one rounding
+    bounded(got, want, 2.0 ** -8 * np.abs(want) if out == torch.bfloat16 else 0)
