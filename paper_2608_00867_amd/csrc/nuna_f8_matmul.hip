@@ -632,18 +632,28 @@ void by_kind(int kind, int out_dtype, F f) {
         typed(std::integral_constant<int, kScaleE8m0>{});
 }
 
+// Whether the rules below ask for a form with this scale kind and output type: the others are not built.
+template <int BY, int BX, int WY, int WX, bool WGRAD>
+constexpr bool asked_for(int kind, int out_dtype) {
+    if (WGRAD && BY == 128) return (WY * WX == 4) == (kind == kScaleF32 && out_dtype == kDtF32);
+    return out_dtype == kDtBf16 || BY * BX < 256 * 256;
+}
+
 template <int BY, int BX, int WY, int WX, int STAGES, bool WGRAD>
 hipError_t launch_tiles(const Operand& Y, const Operand& X, Shape shape, void* out, int kind, int out_dtype,
                         hipStream_t stream) {
     if (!lay_out<BY, BX, WGRAD>(shape)) return hipErrorInvalidValue;
     const int64_t grid = std::min<int64_t>(shape.items, grid_limit(int64_t(1) << 20));
+    hipError_t e = hipErrorInvalidValue;
     by_kind(kind, out_dtype, [&](auto kd, auto od) {
-        if constexpr (decltype(od)::value == kDtBf16 || BY * BX < 256 * 256)
+        if constexpr (asked_for<BY, BX, WY, WX, WGRAD>(decltype(kd)::value, decltype(od)::value)) {
             k_f8_tiles<BY, BX, WY, WX, STAGES, decltype(kd)::value, WGRAD, decltype(od)::value>
                 <<<static_cast<uint32_t>(grid), WY * WX * 64, 0, stream>>>(Y, X, shape, out);
+            note_launch(WGRAD ? "k_f8_tiles_wgrad" : "k_f8_tiles", kMapLinear, 1, grid, WY * WX * 64, 1);
+            e = hipGetLastError();
+        }
     });
-    note_launch(WGRAD ? "k_f8_tiles_wgrad" : "k_f8_tiles", kMapLinear, 1, grid, WY * WX * 64, 1);
-    return hipGetLastError();
+    return e;
 }
 
 template <int YT, int XT, int W>
