@@ -140,6 +140,115 @@ def bounded(got, want, bound, what=""):
         f"{got[bad][0]} for {want[bad][0]}, bound {np.broadcast_to(bound, got.shape)[bad][0]}"
 
 
+# ------------------------------------------------------------------ many groups
+
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+@pytest.mark.parametrize("groups,rows", [(65, 64), (128, 4000), (160, 700), (256, 5000), (1024, 2100)])
+def test_products_of_many_groups(nuna, groups, rows, kind, out):
+    n, k, off = 72, 128, cut_rows(rows, groups, groups)
+    a, sa = nuna.f8_quantize(normal((rows, k), 1).cuda(), kind)
+    b, sb = nuna.f8_quantize_blocks(normal((groups, n, k), 2).cuda(), kind)
+    got = host(nuna.f8_matmul(a, sa, b, sb, offsets=dev(off), out_dtype=out))
+    a64 = values8(a, sa)
+    for g in np.flatnonzero(np.diff(off)):
+        r = slice(off[g], off[g + 1])
+        b64 = values8(b[g], sb[g], 128)
+        want = a64[r] @ b64.T
+        bound = sum_bound(a64[r], b64, k)
+        if out == torch.bfloat16:
+            bound = bound + 2.0 ** -8 * np.abs(want) + cut_bound(a64[r], b64)
+        bounded(got[r], want, bound, f"group {g}")
+
+
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+@pytest.mark.parametrize("groups,rows", [(65, 64), (128, 4000), (160, 700), (256, 5000), (1024, 2100)])
+def test_columns_and_gradient_of_many_groups(nuna, groups, rows, kind):
+    n, k, off = 40, 24, cut_rows(rows, groups, groups + 1)
+    dy, x = normal((rows, n), 3).bfloat16(), normal((rows, k), 4).bfloat16()
+    (a, sa), (b, sb) = (nuna.f8_quantize_cols(t.cuda(), dev(off), kind) for t in (dy, x))
+    for t, q, s in ((dy, a, sa), (x, b, sb)):
+        want_q, want_s = ref.quantize(ref.columns(t.double().numpy(), off, rows), kind)
+        assert np.array_equal(host(q), want_q) and np.array_equal(host(s)[:, :want_s.shape[1]], want_s)
+    got = host(nuna.f8_wgrad(a, sa, b, sb, dev(off)))
+    a64, b64 = values8(a, sa), values8(b, sb)
+    for g in range(groups):
+        at, c = 128 * (off[g] // 128 + g), off[g + 1] - off[g]
+        u, v = a64[:, at:at + c], b64[:, at:at + c]
+        bounded(got[g], u @ v.T, sum_bound(u, v, c), f"group {g}")
+
+
+# ------------------------------------------------------------------ edges of the formats, strides, many choices
+
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+def test_columns_of_bf16_at_the_edges(nuna, kind):
+    """Infinities, NaN, zeros, subnormal and the smallest and largest magnitudes, along the columns of bf16 rows."""
+    x = torch.zeros((256, 14))
+    x[7, 0], x[130, 1], x[3, 2] = float("inf"), float("nan"), float("-inf")
+    x[:, 3], x[:, 4] = 1e-38, 1e-40
+    x[0, 5], x[200, 5] = 3.38e38, -3.38e38
+    x[:, 6], x[:, 7] = 448, -0.0
+    x[:128, 8], x[0, 8] = torch.linspace(0, 0.02, 128), 448
+    x[:, 9] = 2.0 ** -120
+    x[:, 10], x[:, 11] = normal((256,), 1) * 1e-38, normal((256,), 2) * 5e37
+    x[0, 12], x[1, 12] = 1e-38, 2.0 ** -133
+    x[:, 13] = 7
+    x = x.bfloat16()
+    with np.errstate(all="ignore"):
+        want_q, want_s = ref.quantize(x.double().numpy().T, kind)
+    q, s = nuna.f8_quantize_cols(x.cuda(), dev(np.array([0, 256], np.int32)), kind)
+    assert np.array_equal(host(q)[:, :256], want_q, equal_nan=True)
+    assert np.array_equal(host(s)[:, :2], want_s, equal_nan=True)
+    rows_q, rows_s = nuna.f8_quantize(x.t().contiguous().cuda(), kind)
+    assert torch.equal(rows_q.view(torch.uint8), q.view(torch.uint8)[:, :256])  # the sign of zero too
+    assert np.isnan(want_s[0, 0]) and np.isnan(want_s[1, 1]) and np.isfinite(want_s[3:]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,extra", [(200, 3), (128, 8), (257, 31)])
+def test_strided_rows_are_quantised_as_contiguous_ones(nuna, H, extra, dtype):
+    rows, k, groups = 300, 2, 5
+    x = normal((rows, H + extra), 1).to(dtype).cuda()[:, :H]
+    assert not x.is_contiguous()
+    off = dev(cut_rows(rows, groups, 2))
+    for kind in ("f32", "e8m0"):
+        for got, want in zip(nuna.f8_quantize_cols(x, off, kind), nuna.f8_quantize_cols(x.contiguous(), off, kind)):
+            assert torch.equal(got.view(torch.uint8), want.view(torch.uint8))
+        row_of = dev(np.random.default_rng(3).permutation(rows * k).astype(np.int32).reshape(rows, k))
+        new = lambda: (torch.zeros((rows * k, ref.width(H)), dtype=torch.uint8, device="cuda").view(F8),  # noqa: E731
+                       torch.zeros((rows * k, ref.pitch(H)), device="cuda").to(torch.float32 if kind == "f32" else E8M0))
+        for got, want in zip(nuna.moe_gather(x, row_of, *new()), nuna.moe_gather(x.contiguous(), row_of, *new())):
+            assert torch.equal(got.view(torch.uint8), want.view(torch.uint8))
+
+
+@pytest.mark.parametrize("k", [64, 65, 130, 1024])
+def test_tokens_of_many_choices(nuna, k):
+    """More choices than a wave has lanes, among them tokens whose choices of one span are all dropped."""
+    T, H = 5, 264
+    g = np.random.default_rng(k)
+    row_of = g.permutation(T * k).astype(np.int32).reshape(T, k)
+    row_of[g.random((T, k)) < 0.3] = -1
+    row_of[1, :64] = -1
+    row_of[2, 64:] = -1
+    row_of[3] = -1
+    x, y, w = normal((T, H), 1), normal((T * k, H), 2), normal((T, k), 3)
+    here = row_of >= 0
+    rows = row_of[here]
+    out = nuna.moe_gather(x.cuda(), dev(row_of), torch.zeros((T * k, H), device="cuda"))
+    want = np.zeros((T * k, H))
+    want[rows] = np.repeat(x.double().numpy()[:, None], k, 1)[here]
+    assert np.array_equal(host(out), want)
+    y64, w64, d64 = y.double().numpy(), w.double().numpy(), x.double().numpy()
+    terms = np.where(here[:, :, None], w64[:, :, None] * y64[np.maximum(row_of, 0)], 0)
+    bounded(host(nuna.moe_scatter(y.cuda(), dev(row_of), w.cuda())), terms.sum(1), (k + 1) * EPS * np.abs(terms).sum(1))
+    dy, dw = nuna.moe_scatter_grad(x.cuda(), y.cuda(), dev(row_of), w.cuda())
+    want = np.zeros((T * k, H))
+    want[rows] = (w64[:, :, None] * d64[:, None])[here]
+    bounded(host(dy), want, 2.0 ** -23 * np.abs(want))
+    each = np.where(here[:, :, None], y64[np.maximum(row_of, 0)] * d64[:, None], 0)
+    bounded(host(dw), each.sum(2), (H + 1) * EPS * np.abs(each).sum(2))
+
+
 # ------------------------------------------------------------------ what the sums hold
 
 def outliers(rows, k, seed):
@@ -201,3 +310,48 @@ def test_small_blocks_after_a_large_one(nuna, rows, n, kind, out):
     got = host(nuna.f8_matmul(q[0], ones(rows), q[1], ones(-(-n // 128)), out_dtype=out))
     want = np.tile(a.sum(1)[:, None], (1, n))  # of numbers that fp32 holds exactly, bf16 with one rounding
     bounded(got, want, 2.0 ** -8 * np.abs(want) if out == torch.bfloat16 else 0)
+
+
+# ------------------------------------------------------------------ which form runs
+
+# (rows, n, k, groups): rows and columns of a tile and threads of a workgroup, of bf16 and of fp32 results.
+FORMS = [((3, 30001, 256, 1), (16, 64, 256), None), ((13, 200, 640, 1), (16, 16, 512), None),
+         ((29, 1001, 1200, 1), (16, 32, 512), None), ((200, 1021, 1300, 1), (32, 32, 512), None),
+         ((300, 2101, 300, 1), (64, 64, 256), None), ((640, 4203, 384, 16), (64, 128, 256), None),
+         ((1000, 6201, 384, 1), (128, 256, 512), None), ((2100, 6201, 600, 1), (256, 256, 512), (128, 256, 512)),
+         ((2500, 5333, 384, 7), (256, 256, 512), (128, 256, 512))]
+
+
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+@pytest.mark.parametrize("size,tile,wide", FORMS)
+def test_forms_of_the_product(nuna, size, tile, wide, kind, out):
+    """The sizes that test_moe_expert_gpu.py checks the product at reach each of its forms: the launch has the workgroups
+    that tiles of the named size need."""
+    rows, n, k, groups = size
+    by, bx, threads = wide if wide and out == torch.float32 else tile
+    sd = torch.float32 if kind == "f32" else E8M0
+    kp = ref.width(k)
+    zeros = lambda *s: torch.zeros(s, dtype=torch.uint8, device="cuda").view(F8)  # noqa: E731
+    ones = lambda *s: torch.ones((*s, ref.pitch(k)), device="cuda").to(sd)  # noqa: E731
+    off = dev(cut_rows(rows, groups, rows)) if groups > 1 else None
+    lead = (groups,) if groups > 1 else ()
+    nuna.f8_matmul(zeros(rows, kp), ones(rows), zeros(*lead, n, kp), ones(*lead, -(-n // 128)), offsets=off, out_dtype=out)
+    ytiles = rows // by + min(groups, rows) if groups > 1 else -(-rows // by)
+    launch = nuna.last_launch()
+    assert (launch["grid"], launch["threads"]) == (-(-ytiles * -(-n // bx) // 8) * 8, threads)
+
+
+@pytest.mark.parametrize("rows,groups", [(3300, 3), (600, 3)])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+def test_forms_of_the_gradient(nuna, rows, groups, kind, out):
+    n, k = 300, 513
+    by, bx, threads = (256, 128, 512) if rows // groups >= 1024 else (128, 128, 512)
+    if rows // groups < 1024 and kind == "f32" and out == torch.float32:
+        threads = 256
+    off = dev(cut_rows(rows, groups, 1))
+    a, b = (nuna.f8_quantize_cols(torch.zeros((rows, c), device="cuda"), off, kind) for c in (n, k))
+    nuna.f8_wgrad(*a, *b, off, out_dtype=out)
+    launch = nuna.last_launch()
+    assert (launch["grid"], launch["threads"]) == (-(-groups * -(-n // by) * -(-k // bx) // 8) * 8, threads)
