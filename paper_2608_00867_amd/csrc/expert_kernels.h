@@ -7,6 +7,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "moe_sort_plan.h"
+
 namespace nuna {
 
 constexpr int kScaleF32 = 0;
@@ -21,7 +23,6 @@ inline size_t f8_scale_size(int kind) { return kind == kScaleF32 ? 4u : 1u; }
 // Columns of `rows` rows laid out along the rows of `groups` groups.
 inline int64_t f8_t_width(int64_t rows, int64_t groups) { return kF8Block * (rows / kF8Block + groups); }
 
-size_t moe_sort_workspace(int64_t slots, int experts);
 hipError_t launch_moe_sort(const int32_t* topk, int64_t slots, int first, int experts, int32_t* offsets,
                            int32_t* slot_of, int32_t* row_of, void* workspace, hipStream_t stream);
 

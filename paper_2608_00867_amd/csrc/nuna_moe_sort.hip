@@ -28,12 +28,6 @@
 namespace nuna {
 namespace {
 
-constexpr int kSortThreads = 1024;
-constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortChunk = 2048;      // slots of a workgroup where there are several: a multiple of this
-constexpr int kSortMaxChunks = 512;   // workgroups at most, as each adds up all chunks' counts
-constexpr int kSortOneSlots = 8192;   // slots that one workgroup takes alone
-
 // Exclusive prefix sum of v over the workgroup's threads, in thread order; total receives the sum.
 __device__ __forceinline__ int block_exclusive(int v, int* wave_sums, int& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -174,20 +168,7 @@ __global__ void k_sort_none(int experts, int32_t* __restrict__ offsets) {
     for (int e = threadIdx.x; e <= experts; e += blockDim.x) offsets[e] = 0;
 }
 
-// Slots of a workgroup, a multiple of kSortThreads.  Fewer workgroups need less workspace.
-int sort_chunk(int64_t slots, int64_t most_chunks) {
-    if (slots <= kSortOneSlots) return static_cast<int>((slots + kSortThreads - 1) / kSortThreads) * kSortThreads;
-    const int64_t unit = kSortChunk * most_chunks;
-    return static_cast<int>((slots + unit - 1) / unit) * kSortChunk;
-}
-
-int64_t sort_chunks(int64_t slots, int chunk) { return (slots + chunk - 1) / chunk; }
-
 }  // namespace
-
-size_t moe_sort_workspace(int64_t slots, int experts) {
-    return slots <= kSortOneSlots ? 0 : static_cast<size_t>(sort_chunks(slots, sort_chunk(slots, kSortMaxChunks))) * experts * sizeof(int32_t);
-}
 
 hipError_t launch_moe_sort(const int32_t* topk, int64_t slots, int first, int experts, int32_t* offsets,
                            int32_t* slot_of, int32_t* row_of, void* workspace, hipStream_t stream) {
