@@ -635,7 +635,7 @@ void by_kind(int kind, int out_dtype, F f) {
 // Whether the rules below ask for a form with this scale kind and output type: the others are not built.
 template <int BY, int BX, int WY, int WX, bool WGRAD>
 constexpr bool asked_for(int kind, int out_dtype) {
-    if (WGRAD && BY == 128) return (WY * WX == 4) == (kind == kScaleF32 && out_dtype == kDtF32);
+    if (WGRAD) return (WY * WX == 4) == (kind == kScaleF32 && out_dtype == kDtF32);
     return out_dtype == kDtBf16 || BY * BX < 256 * 256;
 }
 
@@ -726,11 +726,12 @@ hipError_t launch_f8_wgrad(const void* a, const void* a_scale, const void* b, co
     // Of groups of few rows the outputs are most of the work, and two smaller workgroups of a compute unit, of 8 waves
     // each, hide each other's stores: 32 groups of 256 rows, n = 2048, k = 7168, fp32 results, 587 us, with 4 waves of
     // 64 x 64 648, with 64 x 128 tiles 648, with 256 x 128 643.  (723 us where the operands' rows are a multiple of
-    // 4 KiB apart: their lines then meet in few of the memory's channels.)  Of many rows the larger tile moves less (8
-    // groups of 4096 rows 492, with 128 x 128 tiles 591).  fp32 scales and fp32 results together take 138 registers, of
-    // which two workgroups of 8 waves do not fit: 4 waves there (784 us in that form, in 8 waves 1065, held to 128
-    // registers 802).
-    if (rows / groups >= 1024) return launch_tiles<256, 128, 4, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
+    // 4 KiB apart: their lines then meet in few of the memory's channels.)  Of many rows no larger tile is faster
+    // throughout.  e8m0, bf16 and fp32 results, us: 8 groups of 4096 rows, n = 2048, k = 7168, 694 and 1133 (256 x 128:
+    // 793 and 1192); 2 groups of 16384, 4096 x 4096, 595 and 926 (559 and 874); 1 of 32768, 8192 x 8192, 2343 and 3868
+    // (2632 and 3586); 1 of 16384, 1024 x 1024, 95 and 135 (121 and 204).  fp32 scales and fp32 results together take 141
+    // registers, of which two workgroups of 8 waves do not fit: 4 waves there (784 us in that form, in 8 waves 1065, held
+    // to 128 registers 802).
     if (kind == kScaleF32 && out_dtype == kDtF32)
         return launch_tiles<128, 128, 2, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);
     return launch_tiles<128, 128, 4, 2, 2, true>(Y, X, shape, out, kind, out_dtype, stream);

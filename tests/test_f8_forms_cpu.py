@@ -16,7 +16,7 @@ ALL = {(s, o) for s in (F32_SCALE, E8M0) for o in (F32_OUT, BF16_OUT)}
 # Rows and columns of a tile, waves along each, stages, weights' gradient: the pairs of scale and result that reach it.
 TILES = {(256, 256, 4, 2, 2, False): {(s, BF16_OUT) for s in (F32_SCALE, E8M0)},
          (128, 256, 2, 4, 3, False): ALL, (64, 128, 2, 2, 3, False): ALL, (64, 64, 2, 2, 4, False): ALL,
-         (256, 128, 4, 2, 2, True): ALL, (128, 128, 2, 2, 2, True): {(F32_SCALE, F32_OUT)},
+         (128, 128, 2, 2, 2, True): {(F32_SCALE, F32_OUT)},
          (128, 128, 4, 2, 2, True): ALL - {(F32_SCALE, F32_OUT)}}
 FEW = {(1, 4, 4): ALL, (1, 1, 8): ALL, (1, 2, 8): ALL, (2, 2, 8): ALL}
 

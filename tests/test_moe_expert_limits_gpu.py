@@ -347,9 +347,7 @@ def test_forms_of_the_product(nuna, size, tile, wide, kind, out):
 @pytest.mark.parametrize("kind", ["f32", "e8m0"])
 def test_forms_of_the_gradient(nuna, rows, groups, kind, out):
     n, k = 300, 513
-    by, bx, threads = (256, 128, 512) if rows // groups >= 1024 else (128, 128, 512)
-    if rows // groups < 1024 and kind == "f32" and out == torch.float32:
-        threads = 256
+    by, bx, threads = 128, 128, 256 if kind == "f32" and out == torch.float32 else 512
     off = dev(cut_rows(rows, groups, 1))
     a, b = (nuna.f8_quantize_cols(torch.zeros((rows, c), device="cuda"), off, kind) for c in (n, k))
     nuna.f8_wgrad(*a, *b, off, out_dtype=out)
