@@ -35,7 +35,7 @@
 // 256 experts, 64 rows in all, n = 4096, k = 7168: 115 us, 7.1 TB/s with what
 // the Infinity Cache holds; one row, one matrix 7.1 us, 4.1 TB/s); of many rows
 // the matrix units share the time with LDS, which reads as many bytes as it can
-// in it (8192^3: 2506 TFLOP/s with e8m0 scales, 2267 with fp32, whose
+// in it (8192^3: 2506 to 2651 TFLOP/s with e8m0 scales, 2267 to 2463 with fp32, whose
 // multiply-adds run beside the products; the library's product with one scale
 // for all reaches 2768).  The weights' gradient of few rows a group is bound
 // by latency between its loads, few products and many stores.
@@ -679,7 +679,9 @@ hipError_t launch_f8_matmul(const void* a, const void* a_scale, const void* b, c
     const Operand X = {static_cast<const uint8_t*>(b), static_cast<const uint8_t*>(b_scale), k, scale_bytes};
     const Shape shape = {offsets, groups, static_cast<int>(rows), static_cast<int>(rows), static_cast<int>(n),
                          static_cast<int>(k / kF8Block), 0, 0, 0};
-    // Which kernel, by the rows of a group (on average, with what the caller has room for) and the number of tiles.
+    // Which kernel, by the rows of a group (on average, with what the caller has room for) and the number of tiles.  Room
+    // for 5 to 8 times the rows in use asks for larger tiles than they need: 32 groups of 32 or 64 rows 202 and 210 us
+    // instead of 169 and 178, of 2, 8, 128 or 512 rows up to 6 % more.
     // Measured on MI355X, k = 7168 and n = 4096 where nothing else is said, us.  A larger tile moves less through the
     // L2 and LDS for each product, as long as there are tiles for the 256 compute units; tiles of few rows leave the
     // matrix units idle but read the weights once all the same.

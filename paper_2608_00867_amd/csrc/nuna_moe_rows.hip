@@ -10,7 +10,8 @@
 // within one workgroup.  They move bytes and are bound by HBM, few rows by
 // the launch: a gather of 4099 x 2880 bf16 to 4 rows each takes 18.8 us
 // (6.3 TB/s), the gradient of 4096 x 7168 bf16 with 4096 rows 32.4 us
-// (4.8 TB/s), a scatter of 64 tokens' 512 rows of 7168 3.5 us.
+// (4.8 TB/s), a scatter of 64 tokens' 512 rows of 7168 3.5 us, of 16384 tokens
+// to 16384 rows (an eighth of the slots) 110 us (4.3 TB/s; without weights 96).
 #include <algorithm>
 
 #include "f8_common.h"
