@@ -353,3 +353,38 @@ def test_forms_of_the_gradient(nuna, rows, groups, kind, out):
     nuna.f8_wgrad(*a, *b, off, out_dtype=out)
     launch = nuna.last_launch()
     assert (launch["grid"], launch["threads"]) == (-(-groups * -(-n // by) * -(-k // bx) // 8) * 8, threads)
+
+
+# ------------------------------------------------------------------ the ends of the range
+
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+@pytest.mark.parametrize("rows,n", [(3, 24), (300, 2101)])
+def test_products_near_the_ends_of_the_range(nuna, rows, n, kind, out):
+    """Blocks with values up to 3.1e38 beside small weights, and scales whose product is as small as 2^-118: results are
+    what they should be, as every value and scale here is a power of two or a few of them."""
+    k = 256
+    x = torch.zeros((rows, k))
+    x[0, :] = 2.0 ** 127          # scale 2^127 / 448, or 2^119
+    x[1, :128], x[1, 128:] = 2.0 ** -60, 2.0 ** -61
+    x[2:, ::16] = 1.75 * 2.0 ** 100
+    a, sa = nuna.f8_quantize(x.cuda(), kind)
+    b, sb = nuna.f8_quantize_blocks(torch.full((n, k), 2.0 ** -40).cuda(), kind)
+    got = host(nuna.f8_matmul(a, sa, b, sb, out_dtype=out))
+    a64, b64 = values8(a, sa), values8(b, sb, 128)
+    want = np.tile((a64 @ b64[:1].T), (1, n))
+    assert np.isfinite(want).all() and (want > 0).all()
+    # 2^-24 for each of two scales, their product and the sum's steps; the values' products are all alike in a run.
+    bounded(got, want, (2.0 ** -8 if out == torch.bfloat16 else 2 * (k + 4) * EPS) * want)
+
+
+def test_fp32_results_of_values_past_bf16_are_infinite(nuna):
+    """As nuna.h says: with power-of-two scales a value that quantising brings to 2^128 is infinite in fp32 results, and
+    not in bf16 ones, whose scales meet in the product."""
+    x = torch.zeros((2, 128))
+    x[0, 3], x[1, 3] = 3.35e38, 3.1e38   # 256 and 240 times 2^120
+    a, sa = nuna.f8_quantize(x.cuda(), "e8m0")
+    b, sb = nuna.f8_quantize_blocks(torch.full((16, 128), 2.0 ** -10).cuda(), "e8m0")
+    wide = nuna.f8_matmul(a, sa, b, sb, out_dtype=torch.float32)
+    assert bool(torch.isinf(wide[0]).all()) and bool((wide[1] == 240 * 2.0 ** 110).all())
+    assert bool((nuna.f8_matmul(a, sa, b, sb)[0].float() == 2.0 ** 118).all())
