@@ -589,6 +589,133 @@ nuna_status_t nuna_f8_wgrad(const void* a, const void* a_scale, const void* b, c
                             nuna_scale_t kind, nuna_dtype_t out_dtype, hipStream_t stream);
 
 /*
+ * Around the expert layer in a transformer block: the norm before it, the
+ * router that writes its tables, the activation between its products, and the
+ * whole layer in one call for a few tokens.  The common rules of the expert
+ * layer hold here too: device memory, capturable calls, indices checked on the
+ * device, fp32 sums in an order that neither timing nor launch shapes change.
+ * Outputs that may be left out are NULL.
+ */
+
+/*
+ * Root-mean-square norm of the rows, with the residual's addition before it:
+ *   z = x + residual, rounded to dtype (z = x where residual is NULL)
+ *   r = 1 / sqrt(sum of z^2 / cols + eps),  y = z * r * weight  in fp32
+ *   x         [rows][x_stride >= cols];  residual [rows][residual_stride >= cols]
+ *   weight    [cols] of weight_dtype, dtype or NUNA_F32
+ *   sum       [rows][sum_stride >= cols], z, written where there is a residual.
+ *             It may be the residual or x itself (same stride).
+ *   out       [rows][cols], y rounded to dtype, or NULL
+ *   q, q_scale  y as an 8-bit matrix with blocks of 1 x 128, as
+ *             nuna_f8_quantize writes one (of the fp32 values), or NULL
+ *   rstd      fp32 [rows], r, or NULL
+ * One of out and q has to be there.  cols <= NUNA_NORM_MAX_COLS
+ * (NUNA_ERR_UNSUPPORTED).  Squares are summed in fp32: a row whose sum of
+ * squares passes 3.4e38 comes out as zeros.
+ *
+ * nuna_rms_norm_grad, with u = weight * dout and zr = z * rstd:
+ *   dx = rstd * (u - zr * (sum of u * zr) / cols) + dsum
+ *   dweight = sum over the rows of dout * zr            (fp32, overwritten)
+ * dx is the gradient of x and of the residual; dsum [rows][cols] (or NULL) is
+ * what reaches z through the residual's own way, and may be dx itself.
+ *   dout, dx  [rows][cols] of dtype;  z [rows][z_stride >= cols], as it was normed
+ *   workspace nuna_rms_norm_grad_workspace bytes, 16-byte aligned
+ */
+#define NUNA_NORM_MAX_COLS 32768
+nuna_status_t nuna_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                            const void* weight, nuna_dtype_t weight_dtype, float eps, size_t rows, size_t cols, void* sum,
+                            int64_t sum_stride, void* out, void* q, void* q_scale, nuna_scale_t kind, float* rstd,
+                            nuna_dtype_t dtype, hipStream_t stream);
+nuna_status_t nuna_rms_norm_grad_workspace(size_t rows, size_t cols, size_t* bytes);
+nuna_status_t nuna_rms_norm_grad(const void* dout, const void* z, int64_t z_stride, const void* weight,
+                                 nuna_dtype_t weight_dtype, const float* rstd, const void* dsum, size_t rows, size_t cols,
+                                 void* dx, float* dweight, void* workspace, size_t workspace_bytes, nuna_dtype_t dtype,
+                                 hipStream_t stream);
+
+/*
+ * Router: of each token's scores the topk largest, and their weights.
+ *   score     NUNA_SCORE_SOFTMAX: p_e = exp(z_e) / sum over all experts of exp(z)
+ *             NUNA_SCORE_SIGMOID: p_e = 1 / (1 + exp(-z_e))
+ *   choice    the largest z_e, or with a bias (sigmoid only) the largest
+ *             p_e + bias_e, formed in fp64; in descending order, the lowest
+ *             expert first among equals.  An expert whose logit (or bias) is
+ *             -infinity is never chosen: where none is left the entry is -1 with
+ *             weight 0, which the table's readers skip.  NaN comes first, and its
+ *             weight is NaN.
+ *   weights   factor * p_j / (sum of p over the chosen) where normalize is set,
+ *             factor * p_j otherwise.  Normalised weights are formed relative to
+ *             the largest chosen score, so they cannot all vanish.
+ *   logits    [tokens][stride >= experts] of dtype;  bias fp32 [experts] or NULL
+ *   topk_idx  int32 [tokens][topk], written;  weights fp32 [tokens][topk], written
+ * 1 <= topk <= experts <= NUNA_MAX_EXPERTS, topk <= NUNA_ROUTE_MAX_TOPK.
+ *
+ * nuna_route_topk_grad is the gradient of the weights by the logits (the choice
+ * and the bias have none), from the logits and topk_idx of the forward call:
+ *   dlogits   [tokens][experts] of dtype, every entry written
+ * Entries of topk_idx outside [0, experts) have no part in it.
+ */
+#define NUNA_ROUTE_MAX_TOPK 64
+typedef enum { NUNA_SCORE_SOFTMAX = 0, NUNA_SCORE_SIGMOID = 1 } nuna_score_t;
+nuna_status_t nuna_route_topk(const void* logits, int64_t stride, const float* bias, int64_t tokens, int experts, int topk,
+                              nuna_score_t score, int normalize, float factor, int32_t* topk_idx, float* weights,
+                              nuna_dtype_t dtype, hipStream_t stream);
+nuna_status_t nuna_route_topk_grad(const float* dweights, const void* logits, int64_t stride, const int32_t* topk_idx,
+                                   int64_t tokens, int experts, int topk, nuna_score_t score, int normalize, float factor,
+                                   void* dlogits, nuna_dtype_t dtype, hipStream_t stream);
+
+/*
+ * SwiGLU, between the two products of an expert: with g the first `inner`
+ * columns of a row of gu and u the others, and s = 1 / (1 + exp(-g)),
+ *   h = g * s * u
+ * and its gradient, in the same places:
+ *   dg = dout * u * s * (1 + g * (1 - s)),  du = dout * g * s
+ *   gu        [rows][2 * inner] of dtype;  dout [rows][inner]
+ *   out       [rows][inner], for the gradient [rows][2 * inner], or NULL
+ *   q, q_scale  the same as an 8-bit matrix with blocks of 1 x 128, as
+ *             nuna_f8_quantize writes one (of the fp32 values), or NULL
+ *   offsets   int32 [groups + 1] as nuna_moe_sort writes them: rows from
+ *             offsets[groups] on are neither read nor written.  NULL: all rows.
+ * One of out and q has to be there.
+ */
+nuna_status_t nuna_swiglu(const void* gu, const int32_t* offsets, int groups, size_t rows, size_t inner, void* out, void* q,
+                          void* q_scale, nuna_scale_t kind, nuna_dtype_t dtype, hipStream_t stream);
+nuna_status_t nuna_swiglu_grad(const void* dout, const void* gu, const int32_t* offsets, int groups, size_t rows,
+                               size_t inner, void* out, void* q, void* q_scale, nuna_scale_t kind, nuna_dtype_t dtype,
+                               hipStream_t stream);
+
+/*
+ * A whole expert layer for a few tokens (a decode step), in two kernels:
+ *   out[t] = sum over j of weights[t][j] * W2[e] SwiGLU(W1[e] x[t]),  e = topk_idx[t][j]
+ * over the entries with an expert in [first_expert, first_expert + num_experts);
+ * a token with none gets zeros.  Every reached expert's weights are read once
+ * for up to 16 tokens; nothing is sorted or gathered.
+ *   x         [tokens][x_stride >= hidden] of dtype
+ *   topk_idx  int32 [tokens][topk], any numbers;  weights fp32 [tokens][topk]
+ *   w1        8-bit [num_experts][2 * inner][kp of hidden], w1_scale
+ *             [num_experts][ceil(2 * inner / 128)][pitch], the gate's rows before
+ *             the others';  w2 [num_experts][hidden][kp of inner] with its scales:
+ *             as nuna_f8_quantize_blocks writes them.  Bytes past a row's last
+ *             column are zeros.
+ *   out       [tokens][hidden] of dtype
+ *   workspace nuna_expert_layer_few_workspace bytes, 16-byte aligned
+ * The tokens are not quantised: products of the 8-bit weights with tokens and
+ * with the activations in fp32 are summed in fp32 (beside bf16 tokens the
+ * activations keep 16 bits), so results are closer to the formula than those of
+ * the 8-bit products.  An expert that a token names twice has the sum of the
+ * weights.  tokens <= NUNA_FEW_TOKENS, topk <= NUNA_FEW_TOPK, hidden and inner
+ * <= NUNA_FEW_MAX_WIDTH (NUNA_ERR_UNSUPPORTED).
+ */
+#define NUNA_FEW_TOKENS 64
+#define NUNA_FEW_TOPK 32
+#define NUNA_FEW_MAX_WIDTH 65536
+nuna_status_t nuna_expert_layer_few_workspace(int tokens, int topk, size_t hidden, size_t inner, size_t* bytes);
+nuna_status_t nuna_expert_layer_few(const void* x, int64_t x_stride, const int32_t* topk_idx, const float* weights,
+                                    int tokens, int topk, const void* w1, const void* w1_scale, const void* w2,
+                                    const void* w2_scale, int first_expert, int num_experts, size_t hidden, size_t inner,
+                                    void* out, void* workspace, size_t workspace_bytes, nuna_scale_t kind,
+                                    nuna_dtype_t dtype, hipStream_t stream);
+
+/*
  * NUNA-aware placement planner: Algorithm 1 of the paper (Sec. 4.2.2,
  * logical allocation then physical placement), host-only, no HIP call.
  *

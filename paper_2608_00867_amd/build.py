@@ -16,8 +16,9 @@ OBJDIR = os.path.join(ROOT, "_build", "libnuna")
 
 SOURCES = [os.path.join(CSRC, f) for f in ("nuna_allreduce.hip", "nuna_rs_ag.hip", "nuna_moe.hip", "nuna_routed.hip",
                                            "nuna_probe.hip", "nuna_moe_sort.hip", "nuna_moe_rows.hip",
-                                           "nuna_f8_quantize.hip", "nuna_f8_matmul.hip", "nap_planner.cpp",
-                                           "nuna_expert_api.cpp", "nuna_api.cpp")]
+                                           "nuna_f8_quantize.hip", "nuna_f8_matmul.hip", "nuna_norm.hip",
+                                           "nuna_router.hip", "nuna_swiglu.hip", "nuna_few.hip", "nap_planner.cpp",
+                                           "nuna_expert_api.cpp", "nuna_block_api.cpp", "nuna_api.cpp")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

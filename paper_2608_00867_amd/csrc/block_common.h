@@ -1,0 +1,103 @@
+// block_common.h -- device helpers of the block's operators: eight values of a
+// row at a time, and sums over the lanes that share a row.
+#pragma once
+
+#include "block_kernels.h"
+#include "f8_common.h"
+
+namespace nuna {
+namespace {
+
+// Eight consecutive values of a row of which the first `n` exist, widened; zeros past them.
+template <int DT>
+__device__ __forceinline__ void load8(const char* p, int64_t n, float (&v)[8]) {
+    constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
+    if (n >= 8) {
+        uint4 raw[8 / L];
+#pragma unroll
+        for (int i = 0; i < 8 / L; ++i) raw[i] = load16_any(p + i * 16);
+#pragma unroll
+        for (int i = 0; i < 8 / L; ++i) Arith<DT>::init(reinterpret_cast<float(&)[L]>(v[i * L]), raw[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = i < n ? Arith<DT>::widen1(*reinterpret_cast<const typename Arith<DT>::Raw*>(p + i * ES)) : 0.0f;
+    }
+}
+
+// The first `n` of eight values, rounded to the type.
+template <int DT>
+__device__ __forceinline__ void store8(char* p, int64_t n, const float (&v)[8]) {
+    constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
+    if (n >= 8) {
+#pragma unroll
+        for (int i = 0; i < 8 / L; ++i)
+            store16_any<false>(p + i * 16, Arith<DT>::narrow(reinterpret_cast<const float(&)[L]>(v[i * L])));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) Arith<DT>::store1(p + i * ES, 0, v[i]);
+    }
+}
+
+// Values as they are after rounding to the type.
+template <int DT>
+__device__ __forceinline__ void round8(float (&v)[8]) {
+    if constexpr (DT == kDtBf16) Arith<DT>::init(v, Arith<DT>::narrow(v));
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+// Sum over each row of 16 lanes, the same in all of them: lanes one apart, two apart, four and eight (turned round).
+__device__ __forceinline__ float sum16(float v) {
+    return dpp_add<0x140>(dpp_add<0x141>(dpp_add<0x4e>(dpp_add<0xb1>(v))));
+}
+
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+    v = max_oct(v);
+    return max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x140, 0xf, 0xf, true)));
+}
+
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
+// Sum over groups of P lanes (16, 32 or 64), the same in all lanes of a group.  All lanes of the wave take part.
+template <int P>
+__device__ __forceinline__ float sum_lanes(float v) {
+    v = sum16(v);
+    if constexpr (P == 16) return v;
+    const float a = lane_value(v, 0) + lane_value(v, 16), b = lane_value(v, 32) + lane_value(v, 48);
+    if constexpr (P == 32) return (threadIdx.x & 32) ? b : a;
+    return a + b;
+}
+
+// 1 / (1 + exp(-g)), within 3 units of fp32's last place from -87 up, 0 below (where it is under 2^-125).  The exponent
+// is kept in two parts, so that its rounding does not grow with g.
+__device__ __forceinline__ float sigmoid(float g) {
+    const float x = -__builtin_amdgcn_fmed3f(g, -87.0f, 87.0f);
+    const float hi = x * 1.44269502f;  // log2(e) = 1.44269502 + 1.9259630e-8
+    const float lo = fmaf(x, 1.9259630e-8f, fmaf(x, 1.44269502f, -hi));
+    float e = __builtin_amdgcn_exp2f(hi);
+    e = fmaf(e, lo * 0.693147182f, e);
+    const float s = __builtin_amdgcn_rcpf(1.0f + e);
+    return g < -87.0f ? 0.0f : s;
+}
+
+// Sum over the workgroup, the same in all threads.  `parts`: LDS for 16 waves' sums, which no earlier call may still be
+// read from.
+__device__ __forceinline__ float sum_workgroup(float v, float* parts) {
+    v = sum_lanes<64>(v);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    if ((threadIdx.x & 63) == 0) parts[wave] = v;
+    __syncthreads();
+    float s = parts[0];
+    for (int i = 1; i < waves; ++i) s += parts[i];
+    return s;
+}
+
+}  // namespace
+}  // namespace nuna

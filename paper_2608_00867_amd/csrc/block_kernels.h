@@ -1,0 +1,125 @@
+// block_kernels.h -- launchers of the operators around the expert layer's in a
+// transformer block (internal to libnuna).  The host API (nuna_block_api.cpp)
+// has validated every argument: pointers non-null and aligned, sizes within
+// range, no overlap but the documented in-place forms.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "expert_kernels.h"
+
+namespace nuna {
+
+// ---------------------------------------------------------------- norm
+
+constexpr int64_t kNormMaxCols = 32768;
+
+struct NormArgs {
+    const void* x;
+    int64_t x_stride;
+    const void* residual;  // or NULL
+    int64_t residual_stride;
+    const void* weight;
+    int weight_dtype;
+    float eps;
+    int64_t rows, cols;
+    void* sum;  // where there is a residual
+    int64_t sum_stride;
+    void* out;  // or NULL
+    void* q;    // or NULL
+    void* q_scale;
+    int kind;
+    float* rstd;  // or NULL
+    int dtype;
+};
+hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream);
+
+struct NormGradArgs {
+    const void* dout;
+    const void* z;
+    int64_t z_stride;
+    const void* weight;
+    int weight_dtype;
+    const float* rstd;
+    const void* dsum;  // or NULL
+    int64_t rows, cols;
+    void* dx;
+    float* dweight;
+    void* workspace;
+    int dtype;
+};
+hipError_t launch_rms_norm_grad(const NormGradArgs& a, hipStream_t stream);
+
+// Rows of partial sums of the weight's gradient at most, one a workgroup.
+constexpr int64_t kNormGradParts = 512;
+inline size_t rms_norm_grad_workspace(int64_t rows, int64_t cols) {
+    return static_cast<size_t>(std::min(rows, kNormGradParts) * cols) * sizeof(float);
+}
+
+// ---------------------------------------------------------------- router
+
+constexpr int kRouteMaxTopk = 64;
+constexpr int kScoreSoftmax = 0;
+constexpr int kScoreSigmoid = 1;
+
+struct RouteArgs {
+    const void* logits;
+    int64_t stride;
+    const float* bias;  // or NULL
+    int64_t tokens;
+    int experts, topk, score;
+    bool normalize;
+    float factor;
+    int dtype;
+};
+hipError_t launch_route_topk(const RouteArgs& a, int32_t* topk_idx, float* weights, hipStream_t stream);
+hipError_t launch_route_topk_grad(const RouteArgs& a, const float* dweights, const int32_t* topk_idx, void* dlogits,
+                                  hipStream_t stream);
+
+// ---------------------------------------------------------------- SwiGLU
+
+struct SwigluArgs {
+    const void* dout;  // of the gradient
+    const void* gu;
+    const int32_t* offsets;  // or NULL
+    int groups;
+    int64_t rows, inner;
+    void* out;  // or NULL
+    void* q;    // or NULL
+    void* q_scale;
+    int kind;
+    int dtype;
+};
+hipError_t launch_swiglu(const SwigluArgs& a, hipStream_t stream);
+hipError_t launch_swiglu_grad(const SwigluArgs& a, hipStream_t stream);
+
+// ---------------------------------------------------------------- expert layer of a few tokens
+
+constexpr int kFewTokens = 64;
+constexpr int kFewTopk = 32;
+constexpr int64_t kFewMaxWidth = 65536;
+
+struct FewArgs {
+    const void* x;
+    int64_t x_stride;
+    const int32_t* topk_idx;
+    const float* weights;
+    int tokens, topk;
+    const void* w1;
+    const void* w1_scale;
+    const void* w2;
+    const void* w2_scale;
+    int first, experts;
+    int64_t hidden, inner;
+    void* out;
+    void* workspace;
+    int kind, dtype;
+};
+size_t expert_layer_few_workspace(int tokens, int topk, int64_t hidden, int64_t inner);
+hipError_t launch_expert_layer_few(const FewArgs& a, hipStream_t stream);
+
+}  // namespace nuna

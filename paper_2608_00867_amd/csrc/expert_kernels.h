@@ -17,7 +17,7 @@ constexpr int kF8Block = 128;
 constexpr int kMaxExperts = 1024;
 
 // Columns of an 8-bit matrix as it is kept, and entries of one of its rows of scales.
-inline int64_t f8_width(int64_t cols) { return (cols + kF8Block - 1) / kF8Block * kF8Block; }
+constexpr int64_t f8_width(int64_t cols) { return (cols + kF8Block - 1) / kF8Block * kF8Block; }
 inline int64_t f8_pitch(int64_t cols) { return (f8_width(cols) / kF8Block + 3) / 4 * 4; }
 inline size_t f8_scale_size(int kind) { return kind == kScaleF32 ? 4u : 1u; }
 // Columns of `rows` rows laid out along the rows of `groups` groups.

@@ -88,6 +88,39 @@ __device__ __forceinline__ uint32_t max_oct(uint32_t v) {
     return max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), 0x141, 0xf, 0xf, true)));  // 7 .. 0
 }
 
+// ---------------------------------------------------------------- values of a row
+
+// Sixteen consecutive values of a row of which the first `n` exist, widened; zeros past them.
+template <int DT>
+__device__ __forceinline__ void load_values(const char* p, int64_t n, float (&v)[16]) {
+    constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
+    if (n >= 16) {
+        uint4 raw[16 / L];
+#pragma unroll
+        for (int i = 0; i < 16 / L; ++i) raw[i] = load16_any(p + i * 16);
+#pragma unroll
+        for (int i = 0; i < 16 / L; ++i) Arith<DT>::init(reinterpret_cast<float(&)[L]>(v[i * L]), raw[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            v[i] = i < n ? Arith<DT>::widen1(*reinterpret_cast<const typename Arith<DT>::Raw*>(p + i * ES)) : 0.0f;
+    }
+}
+
+__device__ __forceinline__ uint32_t max_abs(const float (&v)[16]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max(m, abs_bits(v[i]));
+    return m;
+}
+
+__device__ __forceinline__ uint4 to_e4m3x16(const float (&v)[16], float r) {
+    uint32_t q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = to_e4m3x4(v[4 * i] * r, v[4 * i + 1] * r, v[4 * i + 2] * r, v[4 * i + 3] * r);
+    return make_uint4(q[0], q[1], q[2], q[3]);
+}
+
 // ---------------------------------------------------------------- groups
 
 // Entry i of the offsets, cut to [0, rows].

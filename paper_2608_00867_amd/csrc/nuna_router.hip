@@ -1,0 +1,339 @@
+// nuna_router.hip -- the router of an expert layer: of every token's scores the
+// k largest, and their weights; and the gradient of the weights.
+//
+//   softmax  p_e = exp(z_e) / sum over all experts of exp(z)
+//   sigmoid  p_e = 1 / (1 + exp(-z_e))
+//   choice   the k largest z_e, or p_e + bias_e; the lowest e first among equals
+//   weights  w_j = f p_j / (sum over the chosen of p), or f p_j
+// With q = w / f, g the weights' gradient and <q, g> = sum_j q_j g_j:
+//   softmax, normalised  dz_j = f q_j (g_j - <q, g>) on the chosen, 0 elsewhere
+//   softmax              dz_e = f p_e (g_e - <q, g>), g_e 0 where e was not chosen
+//   sigmoid, normalised  dz_j = f q_j (1 - p_j) (g_j - <q, g>)
+//   sigmoid              dz_j = f g_j p_j (1 - p_j)
+//
+// L lanes hold a token's logits, N consecutive ones each, as integers that
+// order as the numbers do (0: cannot be chosen, or taken).  A choice is the
+// largest of the lanes' largest, of the first lane that has it; only that
+// lane looks for its next largest.  The biased choice compares scores that lie
+// closer together than fp32's sigmoids are exact, so it is made in fp64.
+// Normalised weights do not depend on what all scores have in common, and are
+// formed relative to the largest, so that they cannot vanish together.
+#include <algorithm>
+
+#include "block_common.h"
+
+namespace nuna {
+namespace {
+
+// Order-preserving integers above 0; NaN (the largest, as it should show) by one value, and -0 as 0.
+__device__ __forceinline__ uint32_t order_key(float v) {
+    uint32_t b = __float_as_uint(v + 0.0f);
+    if ((b & 0x7fffffffu) > 0x7f800000u) b = 0x7fc00000u;
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t order_key(double v) {
+    uint64_t b = static_cast<uint64_t>(__double_as_longlong(v + 0.0));
+    if ((b & 0x7fffffffffffffffull) > 0x7ff0000000000000ull) b = 0x7ff8000000000000ull;
+    return b >> 63 ? ~b : b | 0x8000000000000000ull;
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+    return max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), CTRL, 0xf, 0xf, true)));
+}
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp_max(uint64_t v) {
+    const uint32_t lo = __builtin_amdgcn_mov_dpp(static_cast<int>(v), CTRL, 0xf, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_mov_dpp(static_cast<int>(v >> 32), CTRL, 0xf, 0xf, true);
+    return max(v, static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ uint32_t lane_key(uint32_t v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ uint64_t lane_key(uint64_t v, int lane) {
+    return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane))) << 32 |
+           static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), lane));
+}
+
+// Largest over groups of L lanes (16 or 64), the same in all of a group.
+template <int L, class K>
+__device__ __forceinline__ K max_lanes(K v) {
+    v = dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4e>(dpp_max<0xb1>(v))));
+    if constexpr (L == 16) return v;
+    return max(max(lane_key(v, 0), lane_key(v, 16)), max(lane_key(v, 32), lane_key(v, 48)));
+}
+
+template <int DT>
+__device__ __forceinline__ float logit(const void* z, int64_t i) {
+    return Arith<DT>::widen1(static_cast<const typename Arith<DT>::Raw*>(z)[i]);
+}
+
+// N consecutive logits from expert e on; -inf past the last.
+template <int DT, int N>
+__device__ __forceinline__ void load_logits(const void* z, int64_t at, int e, int experts, float (&v)[N]) {
+    constexpr int L = Arith<DT>::kLanes;
+    if (N >= L && e + N <= experts) {
+#pragma unroll
+        for (int i = 0; i < N / L; ++i)
+            Arith<DT>::init(reinterpret_cast<float(&)[L]>(v[i * L]),
+                            load16_any(static_cast<const char*>(z) + (at + e) * Arith<DT>::kEsize + i * 16));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = e + i < experts ? logit<DT>(z, at + e + i) : -__builtin_inff();
+    }
+}
+
+// The sigmoid of z times exp(-common), common <= 0 at least the chosen ones' largest: exp(z - common) / (1 + exp(z)).
+__device__ __forceinline__ float scaled_sigmoid(float z, float common) {
+    return z > 0.0f ? 1.0f / (1.0f + expf(-z)) : expf(z - common) / (1.0f + expf(z));
+}
+
+constexpr float kNegInf = -__builtin_inff();
+
+// A token's chosen logits' scores before they are divided, and what divides them.  z: this lane's slots' logits
+// (-inf: none), in one or more rounds of L lanes.
+template <int L>
+struct Gate {
+    float common;  // what the scores are relative to
+    float total;
+};
+
+template <int DT, int L, int N, bool BIASED>
+__global__ __launch_bounds__(kWG) void k_route_topk(RouteArgs a, int32_t* __restrict__ topk_idx, float* __restrict__ weights) {
+    using Key = std::conditional_t<BIASED, uint64_t, uint32_t>;
+    constexpr int kTokens = kWG / L;
+    __shared__ int picks[kTokens][kRouteMaxTopk];
+    const int lane = threadIdx.x & 63, l = threadIdx.x % L, group = threadIdx.x / L;
+    const int e0 = l * N;
+    const bool softmax = a.score == kScoreSoftmax;
+    for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens; t0 < a.tokens; t0 += static_cast<int64_t>(gridDim.x) * kTokens) {
+        const int64_t token = t0 + group;
+        const int64_t at = token * a.stride;
+        const int experts = token < a.tokens ? a.experts : 0;
+        float z[N];
+        load_logits<DT, N>(a.logits, at, e0, experts, z);
+        Key key[N], best = 0;
+        int best_i = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            bool alive = z[i] != kNegInf;
+            if constexpr (BIASED) {
+                const float b = alive ? a.bias[e0 + i] : kNegInf;
+                alive = alive && b != kNegInf;
+                key[i] = alive ? order_key(1.0 / (1.0 + exp(-static_cast<double>(z[i]))) + static_cast<double>(b)) : 0;
+            } else {
+                key[i] = alive ? order_key(z[i]) : 0;
+            }
+            if (key[i] > best) {
+                best = key[i];
+                best_i = i;
+            }
+        }
+        for (int j = 0; j < a.topk; ++j) {
+            const Key top = max_lanes<L>(best);
+            const uint64_t who = __ballot(best == top) >> (lane / L * L);
+            if (l == __builtin_ctzll(who)) {
+                picks[group][j] = top ? e0 + best_i : -1;
+                best = 0;
+                int next = 0;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    if (i == best_i) key[i] = 0;
+                    if (key[i] > best) {
+                        best = key[i];
+                        next = i;
+                    }
+                }
+                best_i = next;
+            }
+        }
+        // Within a wave LDS needs no barrier: a group's lanes are lanes of one wave.
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float common = 0.0f, total = 1.0f;
+        const auto slot_logit = [&](int j) {
+            const int e = j < a.topk ? picks[group][j] : -1;
+            return e >= 0 && experts ? logit<DT>(a.logits, at + e) : kNegInf;
+        };
+        const auto score = [&](float v) { return softmax ? expf(v - common) : scaled_sigmoid(v, common); };
+        // The chosen's largest logit; without a bias it is the first, and the row's largest.
+        if (softmax || a.normalize) {
+            float m = slot_logit(l);
+            for (int j = l + L; j < a.topk; j += L) m = fmaxf(m, slot_logit(j));
+            const uint32_t k = max_lanes<L>(order_key(m));
+            const float top = __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+            common = top == kNegInf ? 0.0f : softmax ? top : fminf(top, 0.0f);
+            float s = 0.0f;
+            if (a.normalize) {
+                for (int j = l; j < a.topk; j += L) {
+                    const float v = slot_logit(j);
+                    s += v == kNegInf ? 0.0f : score(v);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) s += z[i] == kNegInf ? 0.0f : expf(z[i] - common);
+            }
+            total = sum_lanes<L>(s);
+        }
+        for (int j = l; j < a.topk; j += L) {
+            const float v = slot_logit(j);
+            if (experts) {
+                topk_idx[token * a.topk + j] = picks[group][j];
+                weights[token * a.topk + j] = v == kNegInf ? 0.0f : a.factor * score(v) / total;
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+template <int DT, int L, int N>
+__global__ __launch_bounds__(kWG) void k_route_topk_grad(RouteArgs a, const float* __restrict__ dweights,
+                                                         const int32_t* __restrict__ topk_idx, void* __restrict__ dlogits) {
+    constexpr int kTokens = kWG / L;
+    __shared__ int picks[kTokens][kRouteMaxTopk];
+    __shared__ float parts[kTokens][kRouteMaxTopk];
+    const int l = threadIdx.x % L, group = threadIdx.x / L;
+    const int e0 = l * N;
+    const bool softmax = a.score == kScoreSoftmax, all = softmax && !a.normalize;
+    for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens; t0 < a.tokens; t0 += static_cast<int64_t>(gridDim.x) * kTokens) {
+        const int64_t token = t0 + group;
+        const int64_t at = token * a.stride;
+        const int experts = token < a.tokens ? a.experts : 0;
+        // The chosen's largest logit; a slot without an expert, or whose expert cannot be chosen, has no weight.
+        float m = kNegInf;
+        for (int j = l; j < a.topk; j += L) {
+            int e = experts ? topk_idx[token * a.topk + j] : -1;
+            if (e >= experts || e < 0 || logit<DT>(a.logits, at + e) == kNegInf) e = -1;
+            picks[group][j] = e;
+            if (e >= 0) {
+                const float v = logit<DT>(a.logits, at + e);
+                m = order_key(v) > order_key(m) ? v : m;
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float z[N] = {};
+        if (all) {
+            load_logits<DT, N>(a.logits, at, e0, experts, z);
+#pragma unroll
+            for (int i = 0; i < N; ++i) m = order_key(z[i]) > order_key(m) ? z[i] : m;
+        }
+        float common = 0.0f, total = 1.0f;
+        const auto score = [&](float v) { return softmax ? expf(v - common) : scaled_sigmoid(v, common); };
+        if (softmax || a.normalize) {
+            const uint32_t k = max_lanes<L>(order_key(m));
+            const float top = __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+            common = top == kNegInf ? 0.0f : softmax ? top : fminf(top, 0.0f);
+            float s = 0.0f;
+            if (all) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) s += z[i] == kNegInf ? 0.0f : expf(z[i] - common);
+            } else {
+                for (int j = l; j < a.topk; j += L)
+                    if (picks[group][j] >= 0) s += score(logit<DT>(a.logits, at + picks[group][j]));
+            }
+            total = sum_lanes<L>(s);
+        }
+        float dot = 0.0f;
+        if (softmax || a.normalize) {
+            for (int j = l; j < a.topk; j += L)
+                if (picks[group][j] >= 0)
+                    dot = fmaf(score(logit<DT>(a.logits, at + picks[group][j])) / total, dweights[token * a.topk + j], dot);
+            dot = sum_lanes<L>(dot);
+        }
+        for (int j = l; j < a.topk; j += L) {
+            const int e = picks[group][j];
+            float c = 0.0f;
+            if (e >= 0) {
+                const float v = logit<DT>(a.logits, at + e), g = dweights[token * a.topk + j];
+                if (all)
+                    c = g;
+                else if (a.normalize)
+                    c = a.factor * (score(v) / total) * (softmax ? 1.0f : scaled_sigmoid(-v, 0.0f)) * (g - dot);
+                else
+                    c = a.factor * g * scaled_sigmoid(v, 0.0f) * scaled_sigmoid(-v, 0.0f);
+            }
+            parts[group][j] = c;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float d[N] = {};
+        for (int j = 0; j < a.topk; ++j) {
+            const int i0 = picks[group][j] - e0;
+            const float c = parts[group][j];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i == i0) d[i] += c;
+        }
+        if (all) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                d[i] = z[i] == kNegInf ? 0.0f : a.factor * (expf(z[i] - common) / total) * (d[i] - dot);
+        }
+        char* const to = static_cast<char*>(dlogits) + (token * a.experts + e0) * Arith<DT>::kEsize;
+        if constexpr (N % 8 == 0) {
+#pragma unroll
+            for (int i = 0; i < N; i += 8) store8<DT>(to + i * Arith<DT>::kEsize, experts - e0 - i, reinterpret_cast<const float(&)[8]>(d[i]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (e0 + i < experts) Arith<DT>::store1(to, i, d[i]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// f(lanes a token, logits a lane).
+template <class F>
+void by_experts(const RouteArgs& a, F f) {
+    using std::integral_constant;
+    const auto few = [&](auto l) {
+        constexpr int L = decltype(l)::value;
+        if (a.experts <= L)
+            f(l, integral_constant<int, 1>{});
+        else if (a.experts <= 4 * L)
+            f(l, integral_constant<int, 4>{});
+        else if (a.experts <= 8 * L)
+            f(l, integral_constant<int, 8>{});
+        else
+            f(l, integral_constant<int, 16>{});
+    };
+    if (a.experts <= 256 && a.tokens > 1024)
+        few(integral_constant<int, 16>{});
+    else
+        few(integral_constant<int, 64>{});
+}
+
+template <class F>
+hipError_t by_dtype(int dtype, F f) {
+    if (dtype == kDtF32)
+        f(std::integral_constant<int, kDtF32>{});
+    else
+        f(std::integral_constant<int, kDtBf16>{});
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_route_topk(const RouteArgs& a, int32_t* topk_idx, float* weights, hipStream_t stream) {
+    return by_dtype(a.dtype, [&](auto dt) {
+        by_experts(a, [&](auto lanes, auto each) {
+            constexpr int DT = decltype(dt)::value, L = decltype(lanes)::value, N = decltype(each)::value;
+            const int64_t grid = std::min<int64_t>((a.tokens + kWG / L - 1) / (kWG / L), grid_limit(int64_t(1) << 20));
+            if (a.bias)
+                k_route_topk<DT, L, N, true><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(a, topk_idx, weights);
+            else
+                k_route_topk<DT, L, N, false><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(a, topk_idx, weights);
+            note_launch("k_route_topk", kMapLinear, 1, grid, kWG, 1);
+        });
+    });
+}
+
+hipError_t launch_route_topk_grad(const RouteArgs& a, const float* dweights, const int32_t* topk_idx, void* dlogits,
+                                  hipStream_t stream) {
+    return by_dtype(a.dtype, [&](auto dt) {
+        by_experts(a, [&](auto lanes, auto each) {
+            constexpr int DT = decltype(dt)::value, L = decltype(lanes)::value, N = decltype(each)::value;
+            const int64_t grid = std::min<int64_t>((a.tokens + kWG / L - 1) / (kWG / L), grid_limit(int64_t(1) << 20));
+            k_route_topk_grad<DT, L, N><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(a, dweights, topk_idx, dlogits);
+            note_launch("k_route_topk_grad", kMapLinear, 1, grid, kWG, 1);
+        });
+    });
+}
+
+}  // namespace nuna

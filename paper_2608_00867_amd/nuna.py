@@ -24,8 +24,10 @@ STATUS_NAMES = {0: "NUNA_OK", 1: "NUNA_ERR_INVALID_ARG", 2: "NUNA_ERR_UNSUPPORTE
                 4: "NUNA_ERR_OVERLAP", 5: "NUNA_ERR_HIP", 6: "NUNA_ERR_NO_MEMORY"}
 F32, BF16 = 0, 1
 SCALE_F32, SCALE_E8M0 = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 F8_BLOCK = 128
 MAX_EXPERTS = 1024
+FEW_TOKENS = 64
 LINEAR, XCD = 0, 1
 ALGO_AUTO, ALGO_ONE_SHOT, ALGO_TWO_SHOT, ALGO_ONE_SHOT_SPLIT, ALGO_TWO_SHOT_TWO_KERNELS = 0, 1, 2, 3, 4
 
@@ -118,6 +120,25 @@ SIGNATURES = {
                         ctypes.c_int, ctypes.c_int, _vp], ctypes.c_int),
     "nuna_f8_wgrad": ([_vp, _vp, _vp, _vp, _vp, ctypes.c_int, ctypes.c_size_t, ctypes.c_size_t, ctypes.c_size_t, _vp,
                        ctypes.c_int, ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_rms_norm": ([_vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, ctypes.c_int, ctypes.c_float, ctypes.c_size_t,
+                       ctypes.c_size_t, _vp, ctypes.c_int64, _vp, _vp, _vp, ctypes.c_int, _vp, ctypes.c_int, _vp],
+                      ctypes.c_int),
+    "nuna_rms_norm_grad_workspace": ([ctypes.c_size_t, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)], ctypes.c_int),
+    "nuna_rms_norm_grad": ([_vp, _vp, ctypes.c_int64, _vp, ctypes.c_int, _vp, _vp, ctypes.c_size_t, ctypes.c_size_t, _vp,
+                            _vp, _vp, ctypes.c_size_t, ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_route_topk": ([_vp, ctypes.c_int64, _vp, ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                         ctypes.c_float, _vp, _vp, ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_route_topk_grad": ([_vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                              ctypes.c_int, ctypes.c_float, _vp, ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_swiglu": ([_vp, _vp, ctypes.c_int, ctypes.c_size_t, ctypes.c_size_t, _vp, _vp, _vp, ctypes.c_int, ctypes.c_int,
+                     _vp], ctypes.c_int),
+    "nuna_swiglu_grad": ([_vp, _vp, _vp, ctypes.c_int, ctypes.c_size_t, ctypes.c_size_t, _vp, _vp, _vp, ctypes.c_int,
+                          ctypes.c_int, _vp], ctypes.c_int),
+    "nuna_expert_layer_few_workspace": ([ctypes.c_int, ctypes.c_int, ctypes.c_size_t, ctypes.c_size_t,
+                                         ctypes.POINTER(ctypes.c_size_t)], ctypes.c_int),
+    "nuna_expert_layer_few": ([_vp, ctypes.c_int64, _vp, _vp, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, _vp, ctypes.c_int,
+                               ctypes.c_int, ctypes.c_size_t, ctypes.c_size_t, _vp, _vp, ctypes.c_size_t, ctypes.c_int,
+                               ctypes.c_int, _vp], ctypes.c_int),
     "nuna_placement_items": ([ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, _i64p,
                               ctypes.c_int64, _i64p], ctypes.c_int),
     "nuna_placement_grid": ([ctypes.c_int, ctypes.c_int64, ctypes.c_int64, _i64p], ctypes.c_int),
@@ -940,6 +961,270 @@ def f8_wgrad(a, a_scale, b, b_scale, offsets, out=None, out_dtype=None, stream=N
     _check_tensor(out, "out", (groups, n, k), out_dtype or out.dtype, dev)
     _check(lib().nuna_f8_wgrad(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), offsets.data_ptr(),
                                groups, rows, n, k, out.data_ptr(), kind, _dtype_code(out), _handle(stream, dev)))
+    return out
+
+
+# ------------------------------------------------------------------ around the expert layer
+#
+# As there, all tensors of a call are on the current device, and so is the stream.
+
+SCORES = {"softmax": SCORE_SOFTMAX, "sigmoid": SCORE_SIGMOID}
+
+
+def _f8_wanted(scale, q_out, scale_out):
+    """Whether a call that can also leave its result in 8 bits shall: where a scale type or an output is given.  Returns
+    the scale type, or None."""
+    if scale is None and scale_out is not None:
+        scale = "f32" if _scale_kind(scale_out, "scale_out") == SCALE_F32 else "e8m0"
+    if scale is None and q_out is not None:
+        raise ValueError("q_out needs a scale type, or scale_out")
+    return scale
+
+
+def _check_workspace(workspace, dev):
+    if workspace.get_device() != dev or not workspace.is_contiguous() or workspace.dtype != _torch().uint8:
+        raise ValueError(f"workspace must be a contiguous uint8 CUDA tensor on device {dev}")
+
+
+def _norm_weight(weight, cols, dtype, dev):
+    if weight.dtype is not dtype:
+        dtype = _torch().float32
+    _check_tensor(weight, "weight", (cols,), dtype, dev)
+    return _dtype_code(weight)
+
+
+def rms_norm(x, weight, eps=1e-6, residual=None, residual_out=None, scale=None, out=None, q_out=None, scale_out=None,
+             rstd=None, stream=None):
+    """Root-mean-square norm of the rows of x [T, H] (contiguous rows): x / sqrt(mean(x^2) + eps) * weight.  weight [H]
+    of x's dtype or float32.  With a residual [T, H] it is added to x first; the sum, rounded to x's dtype, is what is
+    normed, and is left in residual_out (the residual itself unless given).  Returns out [T, H]; with a scale type ("f32"
+    or "e8m0") or scale_out, the result in 8 bits (q_out, scale_out) as f8_quantize writes it, and out is written only
+    where it is given.  rstd: a float32 tensor [T] that receives 1 / sqrt(mean + eps), for the gradient."""
+    torch = _torch()
+    dev = _device_of(x, "x")
+    stride = _check_matrix(x, "x", dev)
+    T, H = x.shape
+    wd = _norm_weight(weight, H, x.dtype, dev)
+    rp = sp = None
+    rs = ss = 0
+    if residual is not None:
+        rs = _check_matrix(residual, "residual", dev)
+        residual_out = residual if residual_out is None else residual_out
+        ss = rs if residual_out is residual else _check_matrix(residual_out, "residual_out", dev)
+        for t, name in ((residual, "residual"), (residual_out, "residual_out")):
+            if t.shape != x.shape or t.dtype is not x.dtype:
+                raise ValueError(f"{name} must be {list(x.shape)} of {x.dtype}, got {list(t.shape)} of {t.dtype}")
+        rp, sp = residual.data_ptr(), residual_out.data_ptr()
+    elif residual_out is not None:
+        raise ValueError("residual_out without a residual")
+    scale = _f8_wanted(scale, q_out, scale_out)
+    if scale is not None:
+        q_out, scale_out = _f8_outputs(q_out, scale_out, (T, f8_width(H)), (T, f8_pitch(H)), scale, stream, x.device, dev)
+    elif out is None:
+        out = _new(stream, (T, H), x.dtype, x.device)
+    if out is not None:
+        _check_tensor(out, "out", (T, H), x.dtype, dev)
+    if rstd is not None:
+        _check_tensor(rstd, "rstd", (T,), torch.float32, dev)
+    _check(lib().nuna_rms_norm(x.data_ptr(), stride, rp, rs, weight.data_ptr(), wd, eps, T, H, sp, ss,
+                               None if out is None else out.data_ptr(), None if scale is None else q_out.data_ptr(),
+                               None if scale is None else scale_out.data_ptr(), SCALES[scale or "f32"],
+                               None if rstd is None else rstd.data_ptr(), _dtype_code(x), _handle(stream, dev)))
+    return out if scale is None else (q_out, scale_out)
+
+
+@functools.lru_cache(maxsize=256)
+def rms_norm_grad_workspace(rows, cols):
+    """Bytes of workspace that rms_norm_grad needs."""
+    n = ctypes.c_size_t()
+    _check(lib().nuna_rms_norm_grad_workspace(int(rows), int(cols), ctypes.byref(n)))
+    return n.value
+
+
+def rms_norm_grad(dout, z, weight, rstd, dresidual=None, dx=None, dweight=None, workspace=None, stream=None):
+    """Gradient of rms_norm: (dx, dweight).  z [T, H] (contiguous rows) is what was normed (x, or the sum that residual_out
+    holds), rstd float32 [T] what rms_norm left there.  dx [T, H] is the gradient of x and of the residual alike;
+    dresidual (or None), what reaches the sum by another way, is added to it and may be dx itself.  dweight float32 [H].
+    workspace: a uint8 CUDA tensor of rms_norm_grad_workspace bytes."""
+    torch = _torch()
+    dev = _device_of(z, "z")
+    stride = _check_matrix(z, "z", dev)
+    T, H = z.shape
+    wd = _norm_weight(weight, H, z.dtype, dev)
+    _check_tensor(dout, "dout", (T, H), z.dtype, dev)
+    _check_tensor(rstd, "rstd", (T,), torch.float32, dev)
+    if dresidual is not None:
+        _check_tensor(dresidual, "dresidual", (T, H), z.dtype, dev)
+    need = rms_norm_grad_workspace(T, H)
+    if dx is None:
+        dx = _new(stream, (T, H), z.dtype, z.device)
+    if dweight is None:
+        dweight = _new(stream, (H,), torch.float32, z.device)
+    if workspace is None:
+        workspace = _new(stream, (need,), torch.uint8, z.device)
+    _check_tensor(dx, "dx", (T, H), z.dtype, dev)
+    _check_tensor(dweight, "dweight", (H,), torch.float32, dev)
+    _check_workspace(workspace, dev)
+    _check(lib().nuna_rms_norm_grad(dout.data_ptr(), z.data_ptr(), stride, weight.data_ptr(), wd, rstd.data_ptr(),
+                                    None if dresidual is None else dresidual.data_ptr(), T, H, dx.data_ptr(),
+                                    dweight.data_ptr(), workspace.data_ptr(), workspace.numel(), _dtype_code(z),
+                                    _handle(stream, dev)))
+    return dx, dweight
+
+
+def _score(score):
+    if score not in SCORES:
+        raise ValueError(f"score {score!r} is not one of {sorted(SCORES)}")
+    return SCORES[score]
+
+
+def route_topk(logits, topk, score="softmax", bias=None, normalize=True, factor=1.0, topk_idx=None, weights=None,
+               stream=None):
+    """The router's choice: of each token's scores, "softmax" or "sigmoid" of its logits [T, E] (contiguous rows), the topk
+    largest.  Returns (topk_idx int32 [T, topk], weights float32 [T, topk]), in descending order, the lowest expert first
+    among equals: what moe_sort, all_to_all_routed and moe_scatter take.  bias (float32 [E], sigmoid only) is added to the
+    scores for the choice alone.  weights: the chosen scores, divided by their sum where normalize is set, times factor.
+    An expert whose logit is -inf is never chosen; where none is left the entry is -1 with weight 0."""
+    torch = _torch()
+    dev = _device_of(logits, "logits")
+    stride = _check_matrix(logits, "logits", dev)
+    T, E = logits.shape
+    topk = int(topk)
+    if bias is not None:
+        _check_tensor(bias, "bias", (E,), torch.float32, dev)
+    if topk_idx is None:
+        topk_idx = _new(stream, (T, topk), torch.int32, logits.device)
+    if weights is None:
+        weights = _new(stream, (T, topk), torch.float32, logits.device)
+    _check_tensor(topk_idx, "topk_idx", (T, topk), torch.int32, dev)
+    _check_tensor(weights, "weights", (T, topk), torch.float32, dev)
+    _check(lib().nuna_route_topk(logits.data_ptr(), stride, None if bias is None else bias.data_ptr(), T, E, topk,
+                                 _score(score), int(bool(normalize)), factor, topk_idx.data_ptr(), weights.data_ptr(),
+                                 _dtype_code(logits), _handle(stream, dev)))
+    return topk_idx, weights
+
+
+def route_topk_grad(dweights, logits, topk_idx, score="softmax", normalize=True, factor=1.0, dlogits=None, stream=None):
+    """Gradient of route_topk's weights by the logits, [T, E] of their dtype, from dweights float32 [T, topk] and the
+    topk_idx of the forward call (the choice itself and its bias have no gradient)."""
+    dev = _device_of(logits, "logits")
+    stride = _check_matrix(logits, "logits", dev)
+    T, E = logits.shape
+    rows, k = _check_table(topk_idx, "topk_idx", dev)
+    if rows != T:
+        raise ValueError(f"logits has {T} rows, topk_idx {rows}")
+    _check_tensor(dweights, "dweights", (T, k), _torch().float32, dev)
+    if dlogits is None:
+        dlogits = _new(stream, (T, E), logits.dtype, logits.device)
+    _check_tensor(dlogits, "dlogits", (T, E), logits.dtype, dev)
+    _check(lib().nuna_route_topk_grad(dweights.data_ptr(), logits.data_ptr(), stride, topk_idx.data_ptr(), T, E, k,
+                                      _score(score), int(bool(normalize)), factor, dlogits.data_ptr(),
+                                      _dtype_code(logits), _handle(stream, dev)))
+    return dlogits
+
+
+def _swiglu_outputs(gu, cols, offsets, scale, out, q_out, scale_out, stream, dev):
+    """(groups, scale type or None, out, q_out, scale_out) of swiglu or its gradient: those given, checked, or new ones,
+    zeros where rows of no group are left alone."""
+    rows = gu.shape[0]
+    groups = 0 if offsets is None else _check_offsets(offsets, dev)
+    scale = _f8_wanted(scale, q_out, scale_out)
+    fresh = []
+    if scale is not None:
+        fresh += [name for name, t in (("q", q_out), ("scale", scale_out)) if t is None]
+        q_out, scale_out = _f8_outputs(q_out, scale_out, (rows, f8_width(cols)), (rows, f8_pitch(cols)), scale, stream,
+                                       gu.device, dev)
+    elif out is None:
+        fresh.append("out")
+        out = _new(stream, (rows, cols), gu.dtype, gu.device)
+    if out is not None:
+        _check_tensor(out, "out", (rows, cols), gu.dtype, dev)
+    if offsets is not None and fresh:
+        torch = _torch()
+        with torch.cuda.stream(stream):
+            for name in fresh:
+                {"q": q_out, "scale": scale_out, "out": out}[name].view(torch.uint8).zero_()
+    return groups, scale, out, q_out, scale_out
+
+
+def swiglu(gu, offsets=None, scale=None, out=None, q_out=None, scale_out=None, stream=None):
+    """gate * sigmoid(gate) * up of the halves of gu [rows, 2 * inner]: what stands between an expert's two products.
+    Returns out [rows, inner] of gu's dtype; with a scale type ("f32" or "e8m0") or scale_out, the result in 8 bits (q_out,
+    scale_out) as f8_quantize writes it, and out is written only where it is given.  offsets int32 [groups + 1]
+    (moe_sort): rows in no group are left untouched, and are zeros in outputs that are not given."""
+    dev = _device_of(gu, "gu")
+    if gu.dim() != 2 or gu.shape[1] < 2 or gu.shape[1] % 2:
+        raise ValueError("gu must be [rows, 2 * inner]")
+    rows, inner = gu.shape[0], gu.shape[1] // 2
+    _check_tensor(gu, "gu", (rows, 2 * inner), gu.dtype, dev)
+    groups, scale, out, q_out, scale_out = _swiglu_outputs(gu, inner, offsets, scale, out, q_out, scale_out, stream, dev)
+    _check(lib().nuna_swiglu(gu.data_ptr(), None if offsets is None else offsets.data_ptr(), groups, rows, inner,
+                             None if out is None else out.data_ptr(), None if scale is None else q_out.data_ptr(),
+                             None if scale is None else scale_out.data_ptr(), SCALES[scale or "f32"], _dtype_code(gu),
+                             _handle(stream, dev)))
+    return out if scale is None else (q_out, scale_out)
+
+
+def swiglu_grad(dout, gu, offsets=None, scale=None, out=None, q_out=None, scale_out=None, stream=None):
+    """Gradient of swiglu by gu, [rows, 2 * inner], from dout [rows, inner]; its outputs and offsets as there."""
+    dev = _device_of(gu, "gu")
+    if gu.dim() != 2 or gu.shape[1] < 2 or gu.shape[1] % 2:
+        raise ValueError("gu must be [rows, 2 * inner]")
+    rows, inner = gu.shape[0], gu.shape[1] // 2
+    _check_tensor(gu, "gu", (rows, 2 * inner), gu.dtype, dev)
+    _check_tensor(dout, "dout", (rows, inner), gu.dtype, dev)
+    groups, scale, out, q_out, scale_out = _swiglu_outputs(gu, 2 * inner, offsets, scale, out, q_out, scale_out, stream, dev)
+    _check(lib().nuna_swiglu_grad(dout.data_ptr(), gu.data_ptr(), None if offsets is None else offsets.data_ptr(), groups,
+                                  rows, inner, None if out is None else out.data_ptr(),
+                                  None if scale is None else q_out.data_ptr(),
+                                  None if scale is None else scale_out.data_ptr(), SCALES[scale or "f32"],
+                                  _dtype_code(gu), _handle(stream, dev)))
+    return out if scale is None else (q_out, scale_out)
+
+
+@functools.lru_cache(maxsize=256)
+def expert_layer_few_workspace(tokens, topk, hidden, inner):
+    """Bytes of workspace that expert_layer_few needs."""
+    n = ctypes.c_size_t()
+    _check(lib().nuna_expert_layer_few_workspace(int(tokens), int(topk), int(hidden), int(inner), ctypes.byref(n)))
+    return n.value
+
+
+def expert_layer_few(x, topk_idx, weights, w1, w1_scale, w2, w2_scale, first_expert=0, out=None, workspace=None,
+                     stream=None):
+    """A whole expert layer for up to FEW_TOKENS tokens, in two kernels: out[t] = sum over j of weights[t, j] * w2[e] @
+    swiglu(w1[e] @ x[t]) for e = topk_idx[t, j] - first_expert in [0, experts); a token with none gets zeros.  x [T, H]
+    (contiguous rows), topk_idx int32 and weights float32 [T, k], w1 [experts, 2 * inner, f8_width(H)] and w2 [experts, H,
+    f8_width(inner)] with their scales (f8_quantize_blocks).  The tokens are not quantised.  workspace: a uint8 CUDA tensor
+    of expert_layer_few_workspace bytes, which calls that may run at the same time do not share."""
+    torch = _torch()
+    f8 = torch.float8_e4m3fn
+    dev = _device_of(x, "x")
+    stride = _check_matrix(x, "x", dev)
+    T, H = x.shape
+    rows, k = _check_table(topk_idx, "topk_idx", dev)
+    if rows != T:
+        raise ValueError(f"x has {T} rows, topk_idx {rows}")
+    wp = _check_weights(weights, T, k, dev)
+    if w1.dim() != 3 or w1.shape[1] < 2 or w1.shape[1] % 2:
+        raise ValueError("w1 must be [experts, 2 * inner, f8_width(hidden)]")
+    E, inner = w1.shape[0], w1.shape[1] // 2
+    kind = _scale_kind(w1_scale, "w1_scale")
+    _check_tensor(w1, "w1", (E, 2 * inner, f8_width(H)), f8, dev)
+    _check_tensor(w2, "w2", (E, H, f8_width(inner)), f8, dev)
+    _check_tensor(w1_scale, "w1_scale", (E, -(-2 * inner // F8_BLOCK), f8_pitch(H)), w1_scale.dtype, dev)
+    _check_tensor(w2_scale, "w2_scale", (E, -(-H // F8_BLOCK), f8_pitch(inner)), w1_scale.dtype, dev)
+    need = expert_layer_few_workspace(T, k, H, inner)
+    if out is None:
+        out = _new(stream, (T, H), x.dtype, x.device)
+    if workspace is None:
+        workspace = _new(stream, (need,), torch.uint8, x.device)
+    _check_tensor(out, "out", (T, H), x.dtype, dev)
+    _check_workspace(workspace, dev)
+    _check(lib().nuna_expert_layer_few(x.data_ptr(), stride, topk_idx.data_ptr(), wp, T, k, w1.data_ptr(),
+                                       w1_scale.data_ptr(), w2.data_ptr(), w2_scale.data_ptr(), int(first_expert), E, H,
+                                       inner, out.data_ptr(), workspace.data_ptr(), workspace.numel(), kind,
+                                       _dtype_code(x), _handle(stream, dev)))
     return out
 
 

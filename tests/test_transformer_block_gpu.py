@@ -1,0 +1,662 @@
+"""The operators around the expert layer on the GPU against their definitions in 64 bits (block_ref): the norm, the router,
+SwiGLU, their gradients, and the expert layer of a few tokens, at the sizes, masks and strides where they can go wrong.
+
+Bounds.  Whole numbers are compared for equality.  A rounding to bf16 costs 2^-8 of the value, to fp32 2^-24 = EPS.  A sum
+of a row's n values is formed by threads of at most 32 values, then over 16 lanes, 4 rows of lanes and 16 waves: fewer than
+64 roundings, each of at most EPS of the sum of the magnitudes.  The bounds of each operator stand at its tests.
+
+These tests make streams of their own; the tests that pin the map of workgroups to XCDs come before this file."""
+import numpy as np
+import pytest
+
+import block_ref as blk
+import expert_ref as ref
+from test_moe_expert_gpu import DTYPES, bounded, dev, guarded, host, routing, values
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+EPS = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def nuna():
+    from paper_2608_00867_amd import nuna as n
+    n.init()
+    return n
+
+
+def strided(t, gap, fill=float("nan")):
+    """The same rows in a wider matrix, `fill` between them."""
+    whole = torch.full((t.shape[0], t.shape[1] + gap), fill, dtype=t.dtype, device="cuda")
+    whole[:, :t.shape[1]] = t
+    return whole[:, :t.shape[1]]
+
+
+def check_quantized(q, scale, want, slack, kind, used=None):
+    """(q, scale) hold `want` [rows, cols], whose values may be off by `slack` of themselves before they are quantised: the
+    values to half a step of e4m3, 2^-4 of the value or 2^-10 of the scale; the scales by the rule; zeros and ones past
+    the end."""
+    rows, cols = want.shape
+    used = rows if used is None else used
+    got, s = host(q)[:used], host(scale)[:used]
+    blocks = ref.width(cols) // 128
+    v = np.zeros((used, ref.width(cols)))
+    v[:, :cols] = want[:used]
+    amax = np.abs(v).reshape(used, blocks, 128).max(2)
+    lo, hi = (np.maximum(amax * (1 + f) / 448, ref.MIN) for f in (-slack - 3 * EPS, slack + 3 * EPS))
+    if kind == "e8m0":
+        lo, hi = 2.0 ** np.ceil(np.log2(lo)), 2.0 ** np.ceil(np.log2(hi))
+    assert ((s[:, :blocks] >= lo) & (s[:, :blocks] <= hi)).all()
+    assert (s[:, blocks:] == 1).all()
+    assert (got[:, cols:] == 0).all()
+    each = np.repeat(s[:, :blocks], 128, 1)
+    bounded(got * each, v, (2.0 ** -4 + 2 * slack + 4 * EPS) * np.abs(v) + 2.0 ** -10 * each, "8-bit values")
+
+
+# ------------------------------------------------------------------ norm
+#
+# The sum of squares loses 64 EPS of itself, its root half of that; the quotient, the root and eps 3 EPS more; y two
+# products: 40 EPS of y in all, before its rounding.
+
+NORM_SLACK = 40 * EPS
+WIDTHS = [1, 7, 8, 100, 128, 129, 200, 256, 400, 512, 520, 1000, 1024, 1032, 2880, 4097, 7168, 8192, 8200, 16384, 20001, 32768]
+
+
+@pytest.mark.parametrize("H", WIDTHS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 19])
+def test_norm(nuna, T, H, dtype):
+    x, x64 = values((T, H), dtype, H + T)
+    w, w64 = values((H,), "f32" if H % 3 else dtype, H)
+    out, check = guarded(T, H, DTYPES[dtype], 0x5A)
+    rstd = torch.empty(T, device="cuda")
+    nuna.rms_norm(x, w, 1e-5, out=out, rstd=rstd)
+    check()
+    r = 1 / np.sqrt((x64 ** 2).mean(1, keepdims=True) + 1e-5)
+    want = x64 * r * w64
+    bounded(host(rstd), r[:, 0], NORM_SLACK * r[:, 0], "rstd")
+    bounded(host(out), want, (NORM_SLACK + blk.half_step(dtype) * 1.001) * np.abs(want), "out")
+    again = nuna.rms_norm(x, w, 1e-5)
+    assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("H", [1, 100, 128, 384, 640, 1000, 2888, 7168, 9000, 17000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+@pytest.mark.parametrize("both", [False, True])
+def test_norm_residual_in_8_bits(nuna, H, dtype, kind, both):
+    T = 13
+    x, x64 = values((T, H), dtype, H)
+    res, res64 = values((T, H), dtype, H + 1)
+    w, w64 = values((H,), dtype, H + 2)
+    z = torch.empty_like(res)
+    out = torch.empty_like(res) if both else None
+    q, s = nuna.rms_norm(strided(x, 24), w, residual=strided(res, 8), residual_out=z, scale=kind, out=out)
+    total = x64 + res64
+    # bf16 numbers whose sum does not fit fp32 are rounded twice.
+    bounded(host(z), total, (blk.half_step(dtype) * 1.001 + EPS) * np.abs(total), "sum")
+    z64 = host(z)
+    want = z64 / np.sqrt((z64 ** 2).mean(1, keepdims=True) + 1e-6) * w64
+    check_quantized(q, s, want, NORM_SLACK, kind)
+    if both:
+        bounded(host(out), want, (NORM_SLACK + blk.half_step(dtype) * 1.001) * np.abs(want), "out")
+    # In place, over the residual and over x.
+    for over in ("residual", "x"):
+        xc, rc = x.clone(), res.clone()
+        q2, s2 = nuna.rms_norm(xc, w, residual=rc, residual_out=rc if over == "residual" else xc, scale=kind)
+        assert torch.equal(rc if over == "residual" else xc, z)
+        assert torch.equal(q2.view(torch.uint8), q.view(torch.uint8))
+        assert torch.equal(s2.view(torch.uint8), s.view(torch.uint8))
+    rc = res.clone()
+    nuna.rms_norm(x, w, residual=rc)
+    assert torch.equal(rc, z)
+
+
+def test_norm_rows_that_are_not_finite_stay_apart(nuna):
+    x, x64 = values((6, 300), "bf16", 5)
+    x[1, 7], x[3, 299], x[4] = float("inf"), float("nan"), 0
+    w, w64 = values((300,), "bf16", 6)
+    out = torch.empty_like(x)
+    q, s = nuna.rms_norm(x, w, scale="e8m0", out=out)
+    got, scales = host(out), host(s)
+    assert np.isnan(got[3]).all() and np.isnan(got[1, 7]) and np.isnan(scales[3, :3]).all() and np.isnan(scales[1, 0])
+    assert (got[4] == 0).all() and (host(q)[4] == 0).all()
+    for t in (0, 2, 5):
+        want = x64[t] / np.sqrt((x64[t] ** 2).mean() + 1e-6) * w64
+        bounded(got[t], want, (NORM_SLACK + 2.0 ** -8 * 1.001) * np.abs(want))
+
+
+def test_norm_of_many_rows_and_of_none(nuna):
+    x, x64 = values((5003, 136), "bf16", 1)
+    w, w64 = values((136,), "f32", 2)
+    want = x64 / np.sqrt((x64 ** 2).mean(1, keepdims=True) + 1e-6) * w64
+    bounded(host(nuna.rms_norm(x, w)), want, (NORM_SLACK + 2.0 ** -8 * 1.001) * np.abs(want))
+    assert nuna.rms_norm(x[:0], w).shape == (0, 136)
+    q, s = nuna.rms_norm(x[:0], w, residual=x[:0], residual_out=x[:0].clone(), scale="f32")
+    assert q.shape == (0, 256) and s.shape == (0, 4)
+    dx, dw = nuna.rms_norm_grad(x[:0], x[:0], w, torch.empty(0, device="cuda"))
+    assert dx.shape == (0, 136) and bool((dw == 0).all())
+
+
+# dx: zr is one product off, u one; the sum of u zr 66 EPS of its magnitudes; then five roundings of dx's parts.
+@pytest.mark.parametrize("T,H", [(1, 1), (3, 128), (40, 100), (70, 200), (33, 300), (21, 512), (9, 1000), (5, 1032), (600, 136),
+                                 (17, 2880), (530, 1100), (7, 7168), (3, 8200), (2, 32767)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("residual", [False, True])
+def test_norm_grad(nuna, T, H, dtype, residual):
+    z, z64 = values((T, H), dtype, H)
+    dout, d64 = values((T, H), dtype, H + 1)
+    w, w64 = values((H,), dtype if H % 3 else "f32", H + 2)
+    ds, s64 = values((T, H), dtype, H + 3) if residual else (None, 0.0)
+    rstd = torch.empty(T, device="cuda")
+    nuna.rms_norm(z, w, rstd=rstd)
+    r = host(rstd)[:, None]
+    dx, check = guarded(T, H, DTYPES[dtype], 0x5A)
+    got, dw = nuna.rms_norm_grad(dout, strided(z, 8), w, rstd, dresidual=ds, dx=dx)
+    check()
+    zr, u = z64 * r, d64 * w64
+    want = r * (u - zr * (u * zr).mean(1, keepdims=True)) + s64
+    mag = r * (np.abs(u) + np.abs(zr) * np.abs(u * zr).mean(1, keepdims=True)) + np.abs(s64)
+    bounded(host(got), want, 80 * EPS * mag + blk.half_step(dtype) * 1.001 * np.abs(want), "dx")
+    bounded(host(dw), (d64 * zr).sum(0), (T + 4) * EPS * np.abs(d64 * zr).sum(0), "dweight")
+    again = nuna.rms_norm_grad(dout, z, w, rstd, dresidual=ds)
+    assert torch.equal(again[0], got) and torch.equal(again[1], dw)
+    if residual:  # over the residual's own gradient
+        over = ds.clone()
+        assert nuna.rms_norm_grad(dout, z, w, rstd, dresidual=over, dx=over)[0] is over and torch.equal(over, got)
+
+
+def test_norm_grad_against_differences(nuna):
+    """Central differences of the forward definition in 64 bits, through the residual's addition."""
+    T, H, step = 3, 40, 1e-5
+    x, x64 = values((T, H), "f32", 1)
+    res, res64 = values((T, H), "f32", 2)
+    w, w64 = values((H,), "f32", 3)
+    dout, d64 = values((T, H), "f32", 4)
+    z, rstd = torch.empty_like(x), torch.empty(T, device="cuda")
+    nuna.rms_norm(x, w, residual=res, residual_out=z, rstd=rstd)
+    dx, dw = nuna.rms_norm_grad(dout, z, w, rstd)
+
+    def loss(a, b):
+        s = a + res64
+        return (s / np.sqrt((s ** 2).mean(1, keepdims=True) + 1e-6) * b * d64).sum()
+    rng = np.random.default_rng(0)
+    for _ in range(5):
+        vx, vw = rng.standard_normal((T, H)), rng.standard_normal(H)
+        slope = (loss(x64 + step * vx, w64 + step * vw) - loss(x64 - step * vx, w64 - step * vw)) / (2 * step)
+        got = (host(dx) * vx).sum() + (host(dw) * vw).sum()
+        size = np.abs(host(dx) * vx).sum() + np.abs(host(dw) * vw).sum()
+        assert abs(got - slope) <= 1e-5 * size
+
+
+# ------------------------------------------------------------------ router
+#
+# An exponential of a difference d is off by |d| EPS for the difference and 2 EPS for itself; a sum of n of them by fewer
+# than n roundings; then a quotient and a product.
+
+def logits(T, E, dtype, seed, spread=2.0, masked=0.0):
+    g = np.random.default_rng(seed)
+    z = spread * g.standard_normal((T, E))
+    z[g.random((T, E)) < masked] = -np.inf
+    t = torch.from_numpy(z).to(DTYPES[dtype])
+    return t.cuda(), t.double().numpy()
+
+
+ROUTES = [(1, 1, 1), (1, 8, 256), (64, 8, 256), (5, 3, 7), (33, 16, 16), (9, 20, 64), (40, 4, 100), (7, 64, 300), (6, 10, 512), (5, 8, 1000),
+          (3, 64, 1024), (1500, 2, 9), (1100, 6, 64), (1030, 8, 160), (2051, 8, 256), (1200, 17, 130)]
+
+
+@pytest.mark.parametrize("T,k,E", ROUTES)
+@pytest.mark.parametrize("score,normalize,biased", [("softmax", True, False), ("softmax", False, False), ("sigmoid", True, False),
+                                                    ("sigmoid", False, False), ("sigmoid", True, True)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_route(nuna, T, k, E, score, normalize, biased, dtype):
+    z, z64 = logits(T, E, dtype, T + E, masked=0.2 if E < 200 else 0.0)
+    b = torch.randn(E, generator=torch.Generator().manual_seed(E)) * 0.2 if biased else None
+    idx, check_i = guarded(T, k, torch.int32, 0)
+    w, check_w = guarded(T, k, torch.float32, 0)
+    nuna.route_topk(strided(z, 8), k, score, bias=None if b is None else b.cuda(), normalize=normalize, factor=2.5,
+                    topk_idx=idx, weights=w)
+    check_i()
+    check_w()
+    want = blk.choose(z64, k, None if b is None else b.double().numpy())
+    assert np.array_equal(host(idx), want)
+    _, q = blk.gate(z64, want, score, normalize)
+    span = 20.0  # of the logits
+    bounded(host(w), 2.5 * q, (2 * span + E + 12) * EPS * 2.5 * q, "weights")
+    g = torch.randn((T, k), generator=torch.Generator().manual_seed(T)).cuda()
+    d, check_d = guarded(T, E, DTYPES[dtype], 0x5A)
+    nuna.route_topk_grad(g, strided(z, 16), idx, score, normalize, 2.5, dlogits=d)
+    check_d()
+    g64 = host(g)
+    wantd = blk.route_grad(g64, z64, want, score, normalize, 2.5)
+    p, _ = blk.gate(z64, want, score, normalize)
+    # Magnitudes of what is added: q (or p) times the gradients' magnitudes.
+    mag = np.zeros((T, E))
+    sum_abs = (q * np.abs(g64)).sum(1, keepdims=True)
+    for t in range(T):
+        for j, e in enumerate(want[t]):
+            if e >= 0:
+                mag[t, e] += (q[t, j] if normalize else p[t, e]) * (np.abs(g64[t, j]) + (sum_abs[t, 0] if normalize or score == "softmax" else 0))
+    if score == "softmax" and not normalize:
+        mag += np.where(np.isneginf(z64), 0, p) * sum_abs
+    bounded(host(d), wantd, (4 * span + 2 * E + 32) * EPS * 2.5 * mag + blk.half_step(dtype) * 1.001 * np.abs(wantd), "dlogits")
+
+
+def test_route_ties_go_to_the_lowest_expert(nuna):
+    z = torch.zeros((70, 200), device="cuda")
+    z[:, 5::7] = 1.0
+    z[3] = -0.0
+    for dtype in (torch.float32, torch.bfloat16):
+        idx, w = nuna.route_topk(z.to(dtype), 8)
+        want = blk.choose(z.double().cpu().numpy(), 8)
+        assert np.array_equal(host(idx), want)
+    big, _ = nuna.route_topk(z.repeat(20, 1), 8)
+    assert torch.equal(big, idx.repeat(20, 1))
+    bias = torch.zeros(200, device="cuda")
+    bias[100:] = 1.0
+    idx, _ = nuna.route_topk(z * 0, 8, "sigmoid", bias=bias)
+    assert idx.tolist() == [list(range(100, 108))] * 70
+
+
+def test_route_rows_that_are_masked_or_not_finite(nuna):
+    inf = float("inf")
+    rows = [[-inf] * 6, [1, -inf, -inf, -inf, -inf, 0], [float("nan"), 1, 2, 3, 4, 5], [inf, 1, 2, 3, 4, 5],
+            [-200, -190, -300, -250, -260, -400], [200, 90, 300, 250, 260, 400], [-inf, -inf, 3, -inf, -inf, -inf]]
+    z = torch.tensor(rows, device="cuda")
+    z64 = z.double().cpu().numpy()
+    for score in ("softmax", "sigmoid"):
+        for normalize in (True, False):
+            idx, w = nuna.route_topk(z, 3, score, normalize=normalize)
+            i, w = host(idx), host(w)
+            assert np.array_equal(i, [[-1] * 3, [0, 5, -1], [0, 5, 4], [0, 5, 4], [1, 0, 3], [5, 2, 4], [2, -1, -1]])
+            assert (w[i < 0] == 0).all() and np.isnan(w[2, 0])
+            _, q = blk.gate(z64, i, score, normalize)
+            for t in (0, 1, 4, 5, 6):
+                # 1.2e-38: what fp32 holds; a difference of 500 costs 500 EPS.
+                bounded(w[t], q[t], 1100 * EPS * q[t] + 1.2e-38, f"{score} {normalize} row {t}")
+            g = torch.ones((7, 3), device="cuda")
+            g[:, 1] = -2
+            d = host(nuna.route_topk_grad(g, z, idx, score, normalize=normalize))
+            want = blk.route_grad(host(g), z64, i, score, normalize, 1.0)
+            for t in (0, 1, 4, 5, 6):
+                bounded(d[t], want[t], 1e-3 * np.abs(want[t]).max() + 1.2e-38, f"{score} {normalize} gradient of row {t}")
+            assert (d[0] == 0).all()
+
+
+def test_route_biased_choice_near_a_border(nuna):
+    """Scores that fp32's sigmoids cannot tell apart."""
+    z = torch.full((64, 40), 3.0)
+    z += torch.arange(40).flip(0) * 2.0 ** -21  # steps of fp32's numbers near 3, of which sigmoid(3)'s are 1/22
+    b = torch.zeros(40)
+    idx, _ = nuna.route_topk(z.cuda(), 5, "sigmoid", bias=b.cuda())
+    assert np.array_equal(host(idx), blk.choose(z.double().numpy(), 5, b.double().numpy()))
+
+
+def test_route_grad_against_differences(nuna):
+    T, k, E, step = 4, 3, 12, 1e-6
+    z, z64 = logits(T, E, "f32", 3)
+    g = torch.randn((T, k), generator=torch.Generator().manual_seed(1))
+    for score in ("softmax", "sigmoid"):
+        for normalize in (True, False):
+            idx, _ = nuna.route_topk(z, k, score, normalize=normalize, factor=1.5)
+            d = host(nuna.route_topk_grad(g.cuda(), z, idx, score, normalize=normalize, factor=1.5))
+            i = host(idx)
+            v = np.random.default_rng(2).standard_normal((T, E))
+            f = [1.5 * (blk.gate(z64 + s * step * v, i, score, normalize)[1] * g.double().numpy()).sum() for s in (1, -1)]
+            assert abs((d * v).sum() - (f[0] - f[1]) / (2 * step)) <= 1e-5 * np.abs(d * v).sum()
+
+
+def test_route_grad_takes_any_table(nuna):
+    """Entries outside the experts have no part; one that is named twice has both."""
+    z, z64 = logits(3, 6, "f32", 8)
+    idx = torch.tensor([[-1, 2, 2**31 - 1], [6, -2**31, -7], [4, 4, 1]], dtype=torch.int32, device="cuda")
+    g = torch.randn((3, 3), generator=torch.Generator().manual_seed(4)).cuda()
+    i = np.where((host(idx) < 0) | (host(idx) >= 6), -1, host(idx))
+    for score in ("softmax", "sigmoid"):
+        for normalize in (True, False):
+            want = blk.route_grad(host(g), z64, i, score, normalize, 1.0)
+            got = host(nuna.route_topk_grad(g, z, idx, score, normalize=normalize))
+            bounded(got, want, 200 * EPS * np.abs(host(g)).max() * np.ones_like(want))
+
+
+# ------------------------------------------------------------------ SwiGLU
+#
+# The sigmoid is within 8 EPS of itself (0 below -87, where it is under 1.7e-38); products add 2 EPS each.  In
+# 1 + g (1 - s) the difference is off by 10 EPS, times |g|.
+
+def swiglu_bound(gu64, want, dtype, dout=None):
+    g, u = np.split(gu64, 2, 1)
+    tiny = 2e-36 * (1 + np.abs(u))
+    if dout is None:
+        return 14 * EPS * np.abs(want) + tiny + blk.half_step(dtype) * 1.001 * np.abs(want)
+    s = blk.sigmoid(g)
+    dg = np.abs(dout * u) * (s * (20 + 12 * np.abs(g)) * EPS) + tiny * (1 + np.abs(dout))
+    du = 14 * EPS * np.abs(dout * g * s) + tiny * (1 + np.abs(dout))
+    return np.concatenate([dg, du], 1) + blk.half_step(dtype) * 1.001 * np.abs(want)
+
+
+@pytest.mark.parametrize("rows,inner", [(1, 1), (3, 8), (5, 100), (9, 128), (4, 129), (7, 520), (33, 1024), (6, 1033), (2, 2888), (300, 256)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_swiglu(nuna, rows, inner, dtype):
+    gu, gu64 = values((rows, 2 * inner), dtype, inner)
+    dout, d64 = values((rows, inner), dtype, inner + 1)
+    want, wantd = blk.swiglu(gu64), blk.swiglu_grad(d64, gu64)
+    out, check = guarded(rows, inner, DTYPES[dtype], 0x5A)
+    nuna.swiglu(gu, out=out)
+    check()
+    bounded(host(out), want, swiglu_bound(gu64, want, dtype))
+    d, check = guarded(rows, 2 * inner, DTYPES[dtype], 0x5A)
+    nuna.swiglu_grad(dout, gu, out=d)
+    check()
+    bounded(host(d), wantd, swiglu_bound(gu64, wantd, dtype, d64))
+    for kind in ("f32", "e8m0"):
+        both = torch.empty_like(out)
+        q, s = nuna.swiglu(gu, scale=kind, out=both)
+        assert torch.equal(both, out)
+        # A block's values may be 2e-36 off where the sigmoid vanishes; none is the largest of its block.
+        check_quantized(q, s, want, 14 * EPS, kind)
+        q2, s2 = nuna.swiglu(gu, scale=kind)
+        assert torch.equal(q2.view(torch.uint8), q.view(torch.uint8)) and torch.equal(s2.view(torch.uint8), s.view(torch.uint8))
+        bothd = torch.empty_like(d)
+        q, s = nuna.swiglu_grad(dout, gu, scale=kind, out=bothd)
+        assert torch.equal(bothd, d)
+        # Near the zero of the gate's slope (1 + g (1 - s) = 0) a value may be off by more of itself, but not of its block.
+        amax = np.abs(np.pad(wantd, ((0, 0), (0, -2 * inner % 128)))).reshape(rows, -1, 128).max(2)
+        each = np.repeat(host(s)[:, :amax.shape[1]], 128, 1)[:, :2 * inner]
+        bounded(host(q)[:, :2 * inner] * each, wantd,
+                2.0 ** -4 * np.abs(wantd) + 2.0 ** -10 * each + 2 * (swiglu_bound(gu64, wantd, "f32", d64)), "8-bit gradient")
+        assert (host(q)[:, 2 * inner:] == 0).all() and (host(s)[:, amax.shape[1]:] == 1).all()
+
+
+def test_swiglu_far_values(nuna):
+    """Gates from where the sigmoid vanishes to where it is 1, and what is not finite."""
+    inf = float("inf")
+    gates = [-inf, -1e30, -200, -90, -87, -80, -20, -1.278, -1e-30, 0, 1e-30, 5, 40, 88, 200, 1e30, inf, float("nan")]
+    gu = torch.tensor([gates + [1.0] * len(gates), gates + [-3.0] * len(gates)], device="cuda")
+    d = torch.full((2, len(gates)), 0.5, device="cuda")
+    got, gotd = host(nuna.swiglu(gu)), host(nuna.swiglu_grad(d, gu))
+    with np.errstate(all="ignore"):
+        want, wantd = blk.swiglu(host(gu)), blk.swiglu_grad(host(d), host(gu))
+        fine = np.isfinite(host(gu)[:, :len(gates)])
+        bounded(got[fine], want[fine], (swiglu_bound(host(gu), want, "f32"))[fine])
+        b = swiglu_bound(host(gu), wantd, "f32", host(d))
+        # From 1e30 on, g (1 - s) is 1e30 times a difference that is 0.
+        near = np.concatenate([fine & (np.abs(host(gu)[:, :len(gates)]) <= 200)] * 2, 1)
+        bounded(gotd[near], wantd[near], b[near])
+    assert np.isnan(got[:, 0]).all() and np.isinf(got[:, -2]).all() and np.isnan(got[:, -1]).all()
+    q, s = nuna.swiglu(gu, scale="f32")
+    assert np.isnan(host(s)[:, 0]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("inner", [128, 200])
+def test_swiglu_leaves_rows_of_no_group_alone(nuna, dtype, inner):
+    gu, gu64 = values((40, 2 * inner), dtype, 3)
+    dout, d64 = values((40, inner), dtype, 4)
+    offsets = dev(np.array([0, 5, 5, 23], dtype=np.int32))
+    gu[23:] = float("nan")
+    dout[23:] = float("nan")
+    outs = [torch.full((40, inner), 7.0, dtype=DTYPES[dtype], device="cuda"), torch.full((40, 2 * inner), 7.0, dtype=DTYPES[dtype], device="cuda")]
+    for i, call in enumerate((lambda **a: nuna.swiglu(gu, **a), lambda **a: nuna.swiglu_grad(dout, gu, **a))):
+        n = inner * (i + 1)
+        q = torch.full((40, ref.width(n)), 0x33, dtype=torch.uint8, device="cuda")
+        s = torch.full((40, ref.pitch(n)), 9.0, device="cuda")
+        call(offsets=offsets, out=outs[i], q_out=q.view(torch.float8_e4m3fn), scale_out=s)
+        assert bool((outs[i][23:] == 7).all()) and bool((q[23:] == 0x33).all()) and bool((s[23:] == 9).all())
+        want = blk.swiglu(gu64) if i == 0 else blk.swiglu_grad(d64, gu64)
+        b = swiglu_bound(gu64, want, dtype, None if i == 0 else d64)
+        bounded(host(outs[i])[:23], want[:23], b[:23])
+        fresh_q, fresh_s = call(offsets=offsets, scale="f32")
+        assert torch.equal(fresh_q.view(torch.uint8)[:23], q[:23]) and bool((fresh_q.view(torch.uint8)[23:] == 0).all())
+        assert torch.equal(fresh_s[:23], s[:23]) and bool((fresh_s[23:] == 0).all())
+        fresh = call(offsets=offsets)
+        assert torch.equal(fresh[:23], outs[i][:23]) and bool((fresh[23:] == 0).all())
+    # Offsets past the rows, below 0, and of no rows.
+    for last in (1 << 30, -5, 0):
+        off = dev(np.array([0, last], dtype=np.int32))
+        used = min(max(last, 0), 40)
+        got = nuna.swiglu(gu, offsets=off, out=torch.full((40, inner), 7.0, dtype=DTYPES[dtype], device="cuda"))
+        assert bool((got[used:] == 7).all()) and (used == 0 or bool((got[:23] == outs[0][:23]).all()))
+
+
+def test_swiglu_grad_against_differences(nuna):
+    gu, gu64 = values((3, 50), "f32", 1)
+    dout, d64 = values((3, 25), "f32", 2)
+    d = host(nuna.swiglu_grad(dout, gu))
+    v = np.random.default_rng(3).standard_normal(gu64.shape)
+    f = [(blk.swiglu(gu64 + s * 1e-6 * v) * d64).sum() for s in (1, -1)]
+    assert abs((d * v).sum() - (f[0] - f[1]) / 2e-6) <= 1e-5 * np.abs(d * v).sum()
+
+
+# ------------------------------------------------------------------ expert layer of a few tokens
+
+def experts_of(nuna, E, H, inner, kind, seed):
+    """Weights in 8 bits on the device, and their values in 64 bits."""
+    g = torch.Generator().manual_seed(seed)
+    w1 = (torch.randn((E, 2 * inner, H), generator=g) * H ** -0.5 * torch.exp(0.5 * torch.randn((E, 2 * inner, 1), generator=g))).bfloat16()
+    w2 = (torch.randn((E, H, inner), generator=g) * inner ** -0.5).bfloat16()
+    q1, q2 = nuna.f8_quantize_blocks(w1.cuda(), kind), nuna.f8_quantize_blocks(w2.cuda(), kind)
+    return (*q1, *q2), [np.stack([ref.dequantize(host(q)[e], host(s)[e][:, :q.shape[2] // 128], 128)[:, :k] for e in range(E)])
+                        for (q, s), k in ((q1, H), (q2, inner))]
+
+
+def check_few(nuna, x, x64, idx, w, packed, plain, first, dtype, **args):
+    out = nuna.expert_layer_few(x, dev(idx), w, *packed, first_expert=first, **args)
+    want, bound = blk.few(x64, idx, host(w), *plain, first, 16 if dtype == "bf16" else None)
+    bounded(host(out), want, bound + blk.half_step(dtype) * 1.001 * (np.abs(want) + bound), "layer")
+    return out
+
+
+@pytest.mark.parametrize("T,k,E,first,count,H,inner", [
+    (1, 1, 1, 0, 1, 128, 128), (1, 8, 32, 0, 32, 512, 256), (2, 2, 8, 0, 8, 1, 1), (5, 4, 16, 4, 8, 200, 72), (7, 4, 9, 0, 9, 130, 100),
+    (16, 2, 4, 0, 4, 256, 128), (17, 1, 1, 0, 1, 384, 65), (33, 3, 6, 2, 3, 136, 160), (64, 8, 64, 16, 8, 300, 136),
+    (64, 1, 1, 0, 1, 128, 200), (64, 32, 40, 0, 40, 64, 24), (3, 8, 1000, 0, 1000, 40, 8), (6, 2, 5, 0, 5, 1152, 640), (4, 2, 3, 0, 3, 2880, 328)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["f32", "e8m0"])
+def test_few(nuna, T, k, E, first, count, H, inner, dtype, kind):
+    idx = routing(T, k, E, T + E, 0.1)
+    packed, plain = experts_of(nuna, count, H, inner, kind, H + inner)
+    x, x64 = values((T, H), dtype, T, 0.3)
+    w = torch.randn((T, k), generator=torch.Generator().manual_seed(k)).cuda()
+    out, check = guarded(T, H, DTYPES[dtype], 0x5A)
+    check_few(nuna, strided(x, 8), x64, idx, w, packed, plain, first, dtype, out=out)
+    check()
+    assert torch.equal(nuna.expert_layer_few(x, dev(idx), w, *packed, first_expert=first), out)
+
+
+def test_few_tables_of_any_numbers(nuna):
+    """The same expert twice, all tokens at one expert, none here, and numbers at the ends of int32."""
+    packed, plain = experts_of(nuna, 4, 128, 128, "e8m0", 1)
+    x, x64 = values((40, 128), "bf16", 1, 0.3)
+    w = torch.rand((40, 3), generator=torch.Generator().manual_seed(1)).cuda()
+    same = np.full((40, 3), 2, dtype=np.int32)
+    check_few(nuna, x, x64, same, w, packed, plain, 0, "bf16")
+    mixed = np.array([[-2**31, 2**31 - 1, 1], [3, 3, 0], [-1, -1, -1], [4, 5, 2]] * 10, dtype=np.int32)
+    check_few(nuna, x, x64, mixed, w, packed, plain, 0, "bf16")
+    check_few(nuna, x, x64, mixed, w, packed, plain, 2**31 - 3, "bf16")
+    check_few(nuna, x, x64, mixed, w, packed, plain, -2**31, "bf16")
+    out = nuna.expert_layer_few(x, dev(same), w, *packed, first_expert=100)
+    assert bool((out == 0).all())
+    assert nuna.expert_layer_few(x[:0], dev(same[:0]), w[:0], *packed).shape == (0, 128)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_what_is_not_finite_stays_in_its_token(nuna, dtype):
+    packed, plain = experts_of(nuna, 4, 200, 72, "f32", 1)
+    x, x64 = values((6, 200), dtype, 1, 0.3)
+    idx = routing(6, 2, 4, 1)
+    w = torch.rand((6, 2), generator=torch.Generator().manual_seed(1)).cuda()
+    want = nuna.expert_layer_few(x, dev(idx), w, *packed)
+    x[2, 199], x[4, 0] = float("nan"), float("inf")
+    got = nuna.expert_layer_few(x, dev(idx), w, *packed)
+    for t in (0, 1, 3, 5):
+        assert torch.equal(got[t], want[t])
+    assert bool(got[2].isnan().all()) and not bool(got[4].isfinite().any())
+
+
+def test_few_keeps_fp32(nuna):
+    """Tokens whose low bits matter: the same but for their last 8 bits."""
+    packed, plain = experts_of(nuna, 2, 256, 128, "f32", 5)
+    x, _ = values((2, 256), "f32", 1, 0.3)
+    x[1] = (x[0].view(torch.int32) ^ 0xFF).view(torch.float32)
+    x64 = x.double().cpu().numpy()
+    w = torch.ones((2, 1), device="cuda")
+    check_few(nuna, x, x64, np.zeros((2, 1), np.int32), w, packed, plain, 0, "f32")
+
+
+def test_few_agrees_with_the_sorted_path(nuna):
+    """The layer of a few tokens and the path by sort, gather, products and scatter: the same but for the tokens' and the
+    activations' roundings to e4m3, 2^-4 of a value at most and 0.026 of the 2-norm; four of them pass, and the
+    activation hands the gate's on by 1.1 at most."""
+    T, k, E, H, inner = 24, 4, 16, 512, 384
+    packed, _ = experts_of(nuna, E, H, inner, "e8m0", 2)
+    x, _ = values((T, H), "bf16", 1, 0.3)
+    table, w = nuna.route_topk(torch.randn((T, E), generator=torch.Generator().manual_seed(3)).cuda(), k)
+    few = nuna.expert_layer_few(x, table, w, *packed)
+    offsets, slot_of, row_of = nuna.moe_sort(table, E)
+    xq, xs = nuna.f8_quantize(x, "e8m0")
+    rows = T * k
+    gq = torch.empty((rows, nuna.f8_width(H)), dtype=torch.float8_e4m3fn, device="cuda")
+    gs = torch.empty((rows, nuna.f8_pitch(H)), dtype=torch.float8_e8m0fnu, device="cuda")
+    nuna.moe_gather(x, row_of, gq, gs)
+    gu = nuna.f8_matmul(gq, gs, packed[0], packed[1], offsets=offsets)
+    hq, hs = nuna.swiglu(gu, offsets=offsets, scale="e8m0")
+    y = nuna.f8_matmul(hq, hs, packed[2], packed[3], offsets=offsets)
+    long = nuna.moe_scatter(y, row_of, w)
+    d = (few.double() - long.double()).norm() / few.double().norm()
+    assert d <= 1.1 * 2 * 0.026 * 1.5, float(d)
+
+
+# ------------------------------------------------------------------ launches, streams, graphs
+
+def block(nuna, x, res, norm_w, router_w, packed, scratch):
+    """A decode step's expert block: norm, router's logits, choice, layer."""
+    T = x.shape[0]
+    y = nuna.rms_norm(x, norm_w, residual=res, residual_out=scratch["z"], out=scratch["y"])
+    idx, w = nuna.route_topk(torch.matmul(y.float(), router_w, out=scratch["logits"]), 4, topk_idx=scratch["idx"], weights=scratch["w"])
+    return nuna.expert_layer_few(y, idx, w, *packed, out=scratch["out"], workspace=scratch["ws"])
+
+
+def test_block_captured_and_replayed(nuna):
+    T, E, H, inner = 6, 16, 256, 128
+    packed, _ = experts_of(nuna, E, H, inner, "e8m0", 2)
+    norm_w, _ = values((H,), "bf16", 7)
+    router_w = torch.randn((H, E), generator=torch.Generator().manual_seed(1)).cuda()
+    x, res = values((T, H), "bf16", 1)[0], values((T, H), "bf16", 2)[0]
+
+    def scratch():
+        return dict(z=torch.empty_like(x), y=torch.empty_like(x), logits=torch.empty((T, E), device="cuda"),
+                    idx=torch.empty((T, 4), dtype=torch.int32, device="cuda"), w=torch.empty((T, 4), device="cuda"), out=torch.empty_like(x),
+                    ws=torch.empty(nuna.expert_layer_few_workspace(T, 4, H, inner), dtype=torch.uint8, device="cuda"))
+    a, b = scratch(), scratch()
+    block(nuna, x, res, norm_w, router_w, packed, a)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        block(nuna, x, res, norm_w, router_w, packed, b)
+    for seed in range(5):
+        x.copy_(values((T, H), "bf16", seed + 10)[0])
+        block(nuna, x, res, norm_w, router_w, packed, a)
+        b["ws"].fill_(0xFF)
+        g.replay()
+        torch.cuda.synchronize()
+        for name in ("z", "y", "idx", "w", "out"):
+            assert torch.equal(a[name], b[name]), name
+
+
+def test_gradients_captured_and_replayed(nuna):
+    z, dout, ds = (values((70, 1100), "bf16", i)[0] for i in range(3))
+    w, _ = values((1100,), "bf16", 4)
+    rstd = torch.rand(70, device="cuda") + 0.5
+    lg, _ = logits(70, 32, "f32", 1)
+    idx, _ = nuna.route_topk(lg, 4)
+    g4 = torch.randn((70, 4), device="cuda")
+    gu, dh = values((70, 512), "bf16", 5)[0], values((70, 256), "bf16", 6)[0]
+
+    def run():
+        return (*nuna.rms_norm_grad(dout, z, w, rstd, ds), nuna.route_topk_grad(g4, lg, idx), *nuna.swiglu_grad(dh, gu, scale="f32"))
+    run()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured = run()
+    for seed in range(4):
+        dout.copy_(values((70, 1100), "bf16", 20 + seed)[0])
+        dh.copy_(values((70, 256), "bf16", 30 + seed)[0])
+        g4.normal_()
+        want = run()
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(captured, want):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_results_do_not_depend_on_the_launch_or_the_stream(nuna):
+    T = 50
+    x, w = values((T, 300), "bf16", 1)[0], values((300,), "bf16", 2)[0]
+    wide = values((700, 2000), "bf16", 3)[0]
+    wide_w = values((2000,), "bf16", 4)[0]
+    rstd = torch.rand(700, device="cuda") + 0.5
+    lg, _ = logits(2000, 64, "f32", 1)
+    idx, rw = nuna.route_topk(lg, 4)
+    gu = values((90, 600), "bf16", 5)[0]
+    packed, _ = experts_of(nuna, 64, 300, 72, "f32", 2)
+
+    def run(stream=None):
+        a = dict(stream=stream)
+        i, wt = nuna.route_topk(lg, 4, **a)
+        return [*nuna.rms_norm(x, w, scale="f32", **a), nuna.rms_norm(wide, wide_w, **a), *nuna.rms_norm_grad(wide, wide, wide_w, rstd, **a),
+                *nuna.rms_norm_grad(x, x, w, rstd[:T], **a), i, wt, nuna.route_topk_grad(wt, lg, i, **a), nuna.swiglu(gu, **a), *nuna.swiglu_grad(gu[:, :300].contiguous(), gu, scale="e8m0", **a),
+                nuna.expert_layer_few(x, i[:T], wt[:T], *packed, **a)]
+    want = run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = run(side)
+    side.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    try:
+        for cap in (1, 3):
+            assert nuna.lib().nuna_set_max_workgroups(cap) == 0
+            for n, (a, b) in enumerate(zip(run(), want)):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), (cap, n)
+    finally:
+        nuna.lib().nuna_set_max_workgroups(0)
+
+
+def test_wrong_calls_raise(nuna):
+    x, w = values((4, 64), "bf16", 1)[0], values((64,), "bf16", 2)[0]
+    with pytest.raises(ValueError):
+        nuna.rms_norm(x, w[:32])
+    with pytest.raises(ValueError):
+        nuna.rms_norm(x, w, residual_out=x)
+    with pytest.raises(ValueError):
+        nuna.rms_norm(x, w, residual=x[:2])
+    with pytest.raises(ValueError):
+        nuna.rms_norm(x, w, residual=x.float())
+    with pytest.raises(ValueError):
+        nuna.rms_norm(x, w, scale="f16")
+    with pytest.raises(nuna.NunaError):
+        nuna.rms_norm(x, w, out=x)
+    with pytest.raises(nuna.NunaError):
+        nuna.route_topk(x, 65)
+    with pytest.raises(nuna.NunaError):
+        nuna.route_topk(x, 4, bias=torch.zeros(64, device="cuda"))
+    with pytest.raises(ValueError):
+        nuna.route_topk(x, 4, "relu")
+    with pytest.raises(ValueError):
+        nuna.swiglu(x[:, :63].contiguous())
+    with pytest.raises(ValueError):
+        nuna.swiglu(x, q_out=torch.empty((4, 128), dtype=torch.float8_e4m3fn, device="cuda"))
+    packed, _ = experts_of(nuna, 2, 64, 32, "f32", 1)
+    idx, wt = nuna.route_topk(x[:, :2].contiguous(), 1)
+    with pytest.raises(ValueError):
+        nuna.expert_layer_few(x, idx[:3], wt, *packed)
+    with pytest.raises(ValueError):
+        nuna.expert_layer_few(x, idx, wt, *packed[:2], packed[2][:1], packed[3])
+    with pytest.raises(nuna.NunaError):
+        nuna.expert_layer_few(x, idx, wt, *packed, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    big, many = x.repeat(17, 1), idx.repeat(17, 1)
+    with pytest.raises(nuna.NunaError):
+        nuna.expert_layer_few(big, many, wt.repeat(17, 1), *packed)
