@@ -28,7 +28,6 @@ typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
-constexpr int kWaves = 8;
 constexpr int kTile = 16;
 
 // Eight e4m3 values as bf16, exactly.
@@ -38,14 +37,6 @@ __device__ __forceinline__ bf16x8_t widen8(uint32_t a, uint32_t b) {
     const auto v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false);
     const auto v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
     return bf16x8_t{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
-}
-
-// The fp32 value of a scale.
-template <int KIND>
-__device__ __forceinline__ float scale_value(const uint8_t* scales, int64_t i) {
-    if constexpr (KIND == kScaleF32) return reinterpret_cast<const float*>(scales)[i];
-    const uint32_t e = scales[i];
-    return __uint_as_float(e == 0 ? 0x00400000u : e == 255 ? 0x7fc00000u : e << 23);
 }
 
 // v as a sum of S numbers of 8 bits, the bits of bf16, the first in part[0]: cut toward zero but for the last of two,
@@ -65,38 +56,51 @@ __device__ __forceinline__ void split(float v, uint32_t (&part)[S]) {
     }
 }
 
-// What a workgroup knows of the routing.
+// What a workgroup knows of the routing: the expert of each slot, -1 where it is not here, and the reached experts, in an
+// order of their own.
 struct Routing {
-    int16_t expert[kFewTokens * kFewTopk];  // of each slot, -1 where it is not here
-    uint32_t bits[kMaxExperts / 32];  // reached experts
-    int16_t reached[kMaxExperts];           // ascending
+    int16_t expert[kFewTokens * kFewTopk];
+    uint32_t bits[kMaxExperts / 32];
+    int16_t reached[kMaxExperts];
     int count;
 };
 
-// Fills it in.  The workgroup's threads have to meet before and after it.
+// Fills it in.  Up to 64 slots every wave finds the experts by itself, in the order of their first slots.
 __device__ __forceinline__ void find_experts(const FewArgs& a, Routing& r) {
     const int slots = a.tokens * a.topk;
-    for (int i = threadIdx.x; i < kMaxExperts / 32; i += blockDim.x) r.bits[i] = 0;
-    __syncthreads();
+    const bool few = slots <= 64;
+    if (!few) {
+        for (int i = threadIdx.x; i < kMaxExperts / 32; i += blockDim.x) r.bits[i] = 0;
+        __syncthreads();
+    }
+    int mine = -1;
     for (int i = threadIdx.x; i < slots; i += blockDim.x) {
         const int64_t e = static_cast<int64_t>(a.topk_idx[i]) - a.first;
-        const bool here = e >= 0 && e < a.experts;
-        r.expert[i] = here ? static_cast<int16_t>(e) : -1;
-        if (here) atomicOr(&r.bits[e >> 5], 1u << (e & 31));
+        mine = e >= 0 && e < a.experts ? static_cast<int>(e) : -1;
+        r.expert[i] = static_cast<int16_t>(mine);
+        if (!few && mine >= 0) atomicOr(&r.bits[mine >> 5], 1u << (mine & 31));
     }
-    __syncthreads();
+    if (!few) __syncthreads();
     if (threadIdx.x < 64) {
         const int lane = threadIdx.x;
-        uint32_t word = lane < kMaxExperts / 32 ? r.bits[lane] : 0;
-        int upto = __popc(word);
-        const int own = upto;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int below = __shfl_up(upto, d);
-            if (lane >= d) upto += below;
+        if (few) {
+            bool again = mine < 0;
+            for (int j = 0; j < slots; ++j) again = again || (j < lane && __builtin_amdgcn_readlane(mine, j) == mine);
+            const uint64_t firsts = __ballot(!again);
+            if (!again) r.reached[__popcll(firsts & ((uint64_t(1) << lane) - 1))] = static_cast<int16_t>(mine);
+            if (lane == 0) r.count = __popcll(firsts);
+        } else {
+            uint32_t word = lane < kMaxExperts / 32 ? r.bits[lane] : 0;
+            int upto = __popc(word);
+            const int own = upto;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int below = __shfl_up(upto, d);
+                if (lane >= d) upto += below;
+            }
+            int at = upto - own;
+            for (; word; word &= word - 1) r.reached[at++] = static_cast<int16_t>(lane * 32 + __builtin_ctz(word));
+            if (lane == 63) r.count = upto;
         }
-        int at = upto - own;
-        for (; word; word &= word - 1) r.reached[at++] = static_cast<int16_t>(lane * 32 + __builtin_ctz(word));
-        if (lane == 63) r.count = upto;
     }
     __syncthreads();
 }
@@ -127,56 +131,204 @@ __device__ __forceinline__ Chosen find_tokens(const FewArgs& a, const Routing& r
 struct RawFrag {
     i32x4_t a, b;
 };
-__device__ __forceinline__ RawFrag load_frag(const uint8_t* p) {
-    return {*reinterpret_cast<const i32x4_t*>(p), *reinterpret_cast<const i32x4_t*>(p + 64)};
+
+// A block of 128 of 16 rows of weights as it is read, lane l the 16 bytes l % 8 of row l / 8 and of row 8 + l / 8: eight
+// lanes take a line of memory.  (The matrix instruction's own layout, rows in neighbouring lanes, reads at a quarter of
+// the rate: a line then is asked for by lanes that are 16 apart.)
+struct RawBlock {
+    u32x4_t a, b;
+};
+__device__ __forceinline__ RawBlock load_block(const uint8_t* row0, const uint8_t* row8) {
+    return {*reinterpret_cast<const u32x4_t*>(row0), *reinterpret_cast<const u32x4_t*>(row8)};
+}
+// It is turned in 2 KiB of LDS that are the wave's own; a row's parts are kept in the order part ^ (row % 8), so that the
+// 16 rows that are read together lie in different banks.  A wave's LDS instructions are executed in order.
+__device__ __forceinline__ RawFrag turn(const RawBlock& b, uint8_t* lds) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+    uint8_t* const to = lds + (lane >> 3) * kF8Block + ((lane & 7) ^ (lane >> 3)) * 16;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    *reinterpret_cast<u32x4_t*>(to) = b.a;
+    *reinterpret_cast<u32x4_t*>(to + 8 * kF8Block) = b.b;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const uint8_t* const from = lds + l16 * kF8Block + ((quad ^ (l16 & 7)) * 16);
+    return {*reinterpret_cast<const i32x4_t*>(from), *reinterpret_cast<const i32x4_t*>(lds + ((from - lds) ^ 64))};
 }
 
-// c + the products of 64 values of the block (`half` of it), the same lanes' 16 of both operands.
-__device__ __forceinline__ f32x4_t add_products(const i32x4_t& w, const bf16x8_t (&y)[2], f32x4_t c) {
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[0], w[1]), y[0], c, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2], w[3]), y[1], c, 0, 0, 0);
+// A scale as it is kept.
+template <int KIND>
+__device__ __forceinline__ uint32_t scale_bits(const uint8_t* scales, int64_t i) {
+    if constexpr (KIND == kScaleF32) return reinterpret_cast<const uint32_t*>(scales)[i];
+    return scales[i];
+}
+template <int KIND>
+__device__ __forceinline__ float scale_of_bits(uint32_t e) {
+    if constexpr (KIND == kScaleF32) return __uint_as_float(e);
+    return __uint_as_float(e == 0 ? 0x00400000u : e == 255 ? 0x7fc00000u : e << 23);
 }
 
-// A lane's 16 values of a token from column c on, as S parts; zeros from column `cols` on.
+// All waves meet; what they wrote to LDS before can be read.  Loads under way stay so.
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// A lane's 32 values of a block of a token, or of h, in S parts: two halves of 16, as the weights' are held.
+template <int S>
+struct Tokens {
+    bf16x8_t v[S][2][2];
+};
+
+// The same of a token as they are read: bf16 numbers, or fp32 ones that are yet to be split.
+template <int DT>
+struct RawTokens {
+    uint4 v[2][DT == kDtBf16 ? 2 : 4];
+};
+
+// A lane's values of a block of a token, 16 from column c and 16 from c + 64 on; zeros from column `cols` on.
+template <int DT>
+__device__ __forceinline__ RawTokens<DT> load_tokens(const char* x, int64_t c, int64_t cols) {
+    constexpr int ES = Arith<DT>::kEsize, N = DT == kDtBf16 ? 2 : 4;
+    RawTokens<DT> y;
+    if (c + 80 <= cols) {
+#pragma unroll
+        for (int i = 0; i < 2 * N; ++i) y.v[i / N][i % N] = load16_any(x + (c + i / N * 64) * ES + i % N * 16);
+    } else {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float v[16];
+            load_values<DT>(x + (c + half * 64) * ES, cols - c - half * 64, v);
+#pragma unroll
+            for (int i = 0; i < N; ++i) y.v[half][i] = Arith<DT>::narrow(reinterpret_cast<const float(&)[16 / N]>(v[i * 16 / N]));
+        }
+    }
+    return y;
+}
+
 template <int DT, int S>
-__device__ __forceinline__ void load_token(const char* x, int64_t c, int64_t cols, bf16x8_t (&y)[S][2]) {
+__device__ __forceinline__ Tokens<S> to_parts(const RawTokens<DT>& raw) {
+    Tokens<S> y;
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if constexpr (DT == kDtBf16) {
+                static_assert(S == 1, "bf16 tokens are one part");
+                y.v[0][half][j] = __builtin_bit_cast(bf16x8_t, raw.v[half][j]);
+            } else {
+                float v[8];
+                Arith<DT>::init(reinterpret_cast<float(&)[4]>(v[0]), raw.v[half][2 * j]);
+                Arith<DT>::init(reinterpret_cast<float(&)[4]>(v[4]), raw.v[half][2 * j + 1]);
+                uint32_t u[S][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t lo[S], hi[S];
+                    split<S>(v[2 * i], lo);
+                    split<S>(v[2 * i + 1], hi);
+#pragma unroll
+                    for (int s = 0; s < S; ++s) u[s][i] = hi[s] << 16 | lo[s];
+                }
+#pragma unroll
+                for (int s = 0; s < S; ++s) y.v[s][half][j] = __builtin_bit_cast(bf16x8_t, make_uint4(u[s][0], u[s][1], u[s][2], u[s][3]));
+            }
+        }
+    return y;
+}
+
+// Up to kStaged tokens (rows of h) at an expert pass through LDS: lanes next to each other read a row's bytes once, in one
+// to three instructions a block, and fp32 numbers are split once.  In the matrix instruction's layout 16 lanes would ask
+// for the same bytes, in four to twelve instructions.  A part of a row is 256 bytes, its 16-byte pieces kept in the order
+// piece ^ row.
+constexpr int kStaged = 4;
+template <int S>
+constexpr int kStagedBytes = kStaged * S * 2 * kF8Block;
+
+template <int S>
+__device__ __forceinline__ Tokens<S> staged_tokens(const uint8_t* lds, int row) {
+    const int quad = (threadIdx.x & 63) >> 4;
+    Tokens<S> y;
+#pragma unroll
+    for (int p = 0; p < S; ++p)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                y.v[p][half][j] = *reinterpret_cast<const bf16x8_t*>(lds + (row * S + p) * 2 * kF8Block + (((half * 8 + quad * 2 + j) ^ row) * 16));
+    return y;
+}
+
+// A block of the tokens as it is read: lane l has 16 bytes of row l / 16, of fp32 numbers of the rows l / 32 and 2 + l / 32.
+template <int DT>
+struct StagedBlock {
+    u32x4_t v[DT == kDtBf16 ? 1 : 2];
+};
+template <int DT>
+__device__ __forceinline__ u32x4_t load_piece(const char* x, int64_t c, int64_t cols) {
+    constexpr int L = Arith<DT>::kLanes;
+    if (c + L <= cols) return *reinterpret_cast<const u32x4_any_t*>(x + c * Arith<DT>::kEsize);
+    float v[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+        v[i] = c + i < cols ? Arith<DT>::widen1(reinterpret_cast<const typename Arith<DT>::Raw*>(x)[c + i]) : 0.0f;
+    const uint4 p = Arith<DT>::narrow(v);
+    return u32x4_t{p.x, p.y, p.z, p.w};
+}
+template <int DT, int S>
+__device__ __forceinline__ void stage_tokens(const StagedBlock<DT>& b, uint8_t* lds) {
+    const int lane = threadIdx.x & 63;
     if constexpr (DT == kDtBf16) {
         static_assert(S == 1, "bf16 tokens are one part");
-        uint4 v[2];
-        if (c + 16 <= cols) {
-            v[0] = load16_any(x + c * 2);
-            v[1] = load16_any(x + c * 2 + 16);
-        } else {
-            uint32_t u[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t lo = c + 2 * i < cols ? reinterpret_cast<const uint16_t*>(x)[c + 2 * i] : 0;
-                const uint32_t hi = c + 2 * i + 1 < cols ? reinterpret_cast<const uint16_t*>(x)[c + 2 * i + 1] : 0;
-                u[i] = hi << 16 | lo;
-            }
-            v[0] = make_uint4(u[0], u[1], u[2], u[3]);
-            v[1] = make_uint4(u[4], u[5], u[6], u[7]);
-        }
-        y[0][0] = __builtin_bit_cast(bf16x8_t, v[0]);
-        y[0][1] = __builtin_bit_cast(bf16x8_t, v[1]);
+        *reinterpret_cast<u32x4_t*>(lds + (lane >> 4) * 2 * kF8Block + (((lane & 15) ^ (lane >> 4)) * 16)) = b.v[0];
     } else {
-        float v[16];
-        load_values<kDtF32>(x + c * 4, cols - c, v);
-        uint32_t u[S][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint32_t lo[S], hi[S];
-            split<S>(v[2 * i], lo);
-            split<S>(v[2 * i + 1], hi);
+        for (int i = 0; i < 2; ++i) {
+            const int row = 2 * i + (lane >> 5);
+            float v[4];
+            Arith<DT>::init(v, __builtin_bit_cast(uint4, b.v[i]));
+            uint32_t part[4][S];
 #pragma unroll
-            for (int s = 0; s < S; ++s) u[s][i] = hi[s] << 16 | lo[s];
+            for (int j = 0; j < 4; ++j) split<S>(v[j], part[j]);
+#pragma unroll
+            for (int p = 0; p < S; ++p)
+                *reinterpret_cast<uint2*>(lds + (row * S + p) * 2 * kF8Block + ((((lane & 31) >> 1) ^ row) * 16) + (lane & 1) * 8) =
+                    make_uint2(part[1][p] << 16 | part[0][p], part[3][p] << 16 | part[2][p]);
         }
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                y[s][h] = __builtin_bit_cast(bf16x8_t, make_uint4(u[s][4 * h], u[s][4 * h + 1], u[s][4 * h + 2], u[s][4 * h + 3]));
     }
+}
+
+// The products of a block of 128 of 16 weight rows with 16 tokens.
+template <int S>
+__device__ __forceinline__ f32x4_t block_sum(const RawFrag& w, const Tokens<S>& y) {
+    f32x4_t c = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const i32x4_t& f = half ? w.b : w.a;
+        const bf16x8_t w0 = widen8(f[0], f[1]), w1 = widen8(f[2], f[3]);
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0, y.v[s][half][0], c, 0, 0, 0);
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1, y.v[s][half][1], c, 0, 0, 0);
+        }
+    }
+    return c;
+}
+
+// f(stage, block) for the blocks from..to - 1, the stages in turns from the `turn`-th on, which it moves on.  The stages stay
+// in registers of their own: every place in the turn has code of its own.
+template <class Stage, class F>
+__device__ __forceinline__ void turns(Stage& s0, Stage& s1, int from, int to, F f) {
+#pragma nounroll
+    for (int b = from;;) {
+        f(s0, b);
+        if (++b == to) break;
+        f(s1, b);
+        if (++b == to) break;
+    }
+}
+template <class Stage, class F>
+__device__ __forceinline__ void in_turns(Stage (&s)[2], int& turn, int from, int to, F f) {
+    if (from >= to) return;
+    if (turn == 0)
+        turns(s[0], s[1], from, to, f);
+    else
+        turns(s[1], s[0], from, to, f);
+    turn ^= (to - from) & 1;
 }
 
 // Parts of a token's values, and of h.
@@ -185,15 +337,22 @@ constexpr int kXParts = DT == kDtBf16 ? 1 : 3;
 template <int DT>
 constexpr int kHParts = DT == kDtBf16 ? 2 : 3;
 
-// h: work item (reached expert, 16 columns).  The workgroup's waves split the blocks of x among them.
-// h is kept as [slot][part][width], bf16, width = inner to whole blocks, zeros past inner.
-template <int DT, int KIND>
-__global__ __launch_bounds__(kWaves * 64) void k_few_up(FewArgs a, uint16_t* __restrict__ h) {
+constexpr int kWaves = 8;
+static_assert(kFewMaxWidth <= 64 * kWaves * kF8Block, "a lane for each of a wave's blocks");
+
+// h: work item (reached expert, 16 columns).  The workgroup's waves split the blocks of x among them; a wave has its next
+// blocks under way, of the next item where this one has no more.  The weights of a block pass all YT tiles of 16 tokens
+// that can be at one expert.  h is kept as [slot][part][width], bf16, width = inner to whole blocks, zeros past inner.
+template <int DT, int KIND, int YT>
+__global__ __launch_bounds__(kWaves * 64, 2) void k_few_up(FewArgs a, uint16_t* __restrict__ h) {
     constexpr int S = kXParts<DT>, HS = kHParts<DT>;
+    constexpr int kSS = KIND == kScaleF32 ? 4 : 1;
     __shared__ Routing routing;
     __shared__ int tokens[kFewTokens], slots[kFewTokens];
     __shared__ float weights[kFewTokens];
-    __shared__ float sums[kWaves][kTile][2 * kTile + 4];
+    __shared__ __align__(16) float sums[kWaves][kTile][2 * kTile + 4];
+    __shared__ __align__(16) uint8_t turning[kWaves][2][kTile * kF8Block];
+    __shared__ __align__(16) uint8_t staged[kWaves][kStagedBytes<S>];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     find_experts(a, routing);
@@ -201,158 +360,351 @@ __global__ __launch_bounds__(kWaves * 64) void k_few_up(FewArgs a, uint16_t* __r
     const int64_t width = f8_width(a.inner), kp = static_cast<int64_t>(blocks) * kF8Block;
     const int64_t pitch = (blocks + 3) / 4 * 4;
     const int64_t scale_rows = (2 * a.inner + kF8Block - 1) / kF8Block;
-    const int tiles = static_cast<int>(width / kTile);
+    const int tiles = static_cast<int>(width / kTile), items = routing.count * tiles;
     const int per = (blocks + kWaves - 1) / kWaves;
-    const int kb0 = wave * per, kb1 = min(kb0 + per, blocks);
-    constexpr int kSS = KIND == kScaleF32 ? 4 : 1;
-    for (int item = blockIdx.x; item < routing.count * tiles; item += gridDim.x) {
-        const int e = routing.reached[item / tiles];
-        const int64_t c0 = static_cast<int64_t>(item % tiles) * kTile;
-        const Chosen mine = find_tokens(a, routing, e);
-        const int n = mine.n;
-        __syncthreads();  // the last item's tables and sums have been read
-        if (wave == 0 && mine.here) {
-            tokens[mine.rank] = lane;
-            slots[mine.rank] = mine.slot;
-            weights[mine.rank] = mine.weight;
-        }
-        __syncthreads();
-        const uint8_t* const w1 = static_cast<const uint8_t*>(a.w1) + e * 2 * a.inner * kp;
-        const uint8_t* const gate = w1 + min(c0 + l16, a.inner - 1) * kp + quad * 16;
-        const uint8_t* const up = gate + a.inner * kp;
-        // Gate columns share a block's scale; the up ones may lie on both sides of a block's end.
+    const int kb0 = min(wave * per, blocks), kb1 = min(kb0 + per, blocks);
+    const int64_t to_up = a.inner * kp;
+
+    struct Stage {
+        RawBlock g, u;
+    };
+    // The next block to load: its item, and where that lies.  (What is loaded in a branch, or copied before it is used, the
+    // compiler waits for at once: so past the last item its blocks are loaded again, into registers that nothing else takes
+    // the place of.)
+    // A workgroup's items lie together, so that most of them are of the expert before.  With more tokens, where experts of
+    // many cost more than those of few, they are dealt out one by one (64 tokens at 32 of 256 experts: 156 us, together 169).
+    const int grid = static_cast<int>(gridDim.x), wg = static_cast<int>(blockIdx.x);
+    const int item0 = YT > 1 ? wg : static_cast<int>(static_cast<int64_t>(items) * wg / grid);
+    const int item1 = YT > 1 ? items : static_cast<int>(static_cast<int64_t>(items) * (wg + 1) / grid);
+    const int step = YT > 1 ? grid : 1;
+    int next_item = item0, next_kb = kb0;
+    const uint8_t* next_w = static_cast<const uint8_t*>(a.w1);
+    uint32_t row0 = 0, row8 = 0;  // this lane's parts of the rows, in a matrix of less than 2^32 bytes
+    const auto enter = [&](int item) {
+        const int r = item / tiles;
+        const int64_t e = __builtin_amdgcn_readfirstlane(routing.reached[r]);
+        const int64_t c0 = static_cast<int64_t>(item - r * tiles) * kTile;
+        next_w = static_cast<const uint8_t*>(a.w1) + e * 2 * to_up;
+        row0 = static_cast<uint32_t>(min(c0 + (lane >> 3), a.inner - 1) * kp) + (lane & 7) * 16;
+        row8 = static_cast<uint32_t>(min(c0 + 8 + (lane >> 3), a.inner - 1) * kp) + (lane & 7) * 16;
+    };
+    // An item's scales, lane i those of the wave's i-th block.  Gate columns share a block's scale; the up ones may lie on
+    // both sides of a block's end.
+    struct Scales {
+        uint32_t g, u, u2;
+    };
+    const auto scales_of = [&](int item) {
+        const int r = item / tiles;
+        const int64_t e = __builtin_amdgcn_readfirstlane(routing.reached[r]);
+        const int64_t c0 = min(static_cast<int64_t>(item - r * tiles) * kTile, a.inner - 1), up0 = a.inner + c0;
+        const int64_t kb = min(kb0 + lane, blocks - 1);
         const uint8_t* const ws = static_cast<const uint8_t*>(a.w1_scale) + e * scale_rows * pitch * kSS;
-        const int64_t up0 = a.inner + c0, up_block = up0 / kF8Block;
-        const int64_t up_block2 = min((up0 + kTile - 1) / kF8Block, scale_rows - 1);
-        const uint8_t* const gate_scale = ws + min(c0, a.inner - 1) / kF8Block * pitch * kSS;
-        const uint8_t* const up_scale = ws + min(up_block, scale_rows - 1) * pitch * kSS;
-        const uint8_t* const up_scale2 = ws + up_block2 * pitch * kSS;
-        const int in_first = static_cast<int>((up_block + 1) * kF8Block - up0) - quad * 4;  // of this lane's four
-        for (int y0 = 0; y0 < n; y0 += kTile) {
-            const char* const x = static_cast<const char*>(a.x) +
-                                  tokens[min(y0 + l16, n - 1)] * a.x_stride * Arith<DT>::kEsize;
-            f32x4_t ag = {0.0f, 0.0f, 0.0f, 0.0f}, au = ag;
-            if (c0 < a.inner) {
-                for (int kb = kb0; kb < kb1; ++kb) {
-                    const int64_t k = static_cast<int64_t>(kb) * kF8Block;
-                    const RawFrag fg = load_frag(gate + k), fu = load_frag(up + k);
-                    const float sg = scale_value<KIND>(gate_scale, kb);
-                    const float su = scale_value<KIND>(up_scale, kb), su2 = scale_value<KIND>(up_scale2, kb);
-                    f32x4_t pg = {0.0f, 0.0f, 0.0f, 0.0f}, pu = pg;
+        return Scales{scale_bits<KIND>(ws + c0 / kF8Block * pitch * kSS, kb), scale_bits<KIND>(ws + up0 / kF8Block * pitch * kSS, kb),
+                      scale_bits<KIND>(ws + min((up0 + kTile - 1) / kF8Block, scale_rows - 1) * pitch * kSS, kb)};
+    };
+    const auto load = [&](Stage& s) {
+        const uint8_t* const g = next_w + static_cast<int64_t>(next_kb) * kF8Block;
+        const uint8_t* const u = g + to_up;
+        s.g = load_block(g + row0, g + row8);
+        s.u = load_block(u + row0, u + row8);
+        if (++next_kb == kb1) {
+            next_kb = kb0;
+            next_item += step;
+            if (next_item < item1) enter(next_item);
+        }
+    };
+    Stage stages[2];
+    int turn_at = 0;  // the stage that the next block is in
+    Scales scales = {};
+    if (item0 < item1) {
+        enter(item0);
+        scales = scales_of(item0);
+        if (kb0 < kb1) {
+            load(stages[0]);
+            load(stages[1]);
+        }
+    }
+    constexpr int kLoads = DT == kDtBf16 ? 1 : 2, kLanes = 64 * kLoads / kStaged;  // of a block of x: loads, lanes of a row
+    const char* mine_x[kLoads];
+    int r_now = -1, n = 0;  // the expert that the tables and the staged tokens are of
+    for (int item = item0; item < item1; item += step) {
+        const int r = item / tiles;
+        const int64_t c0 = static_cast<int64_t>(item - r * tiles) * kTile;
+        const float sg = scale_of_bits<KIND>(scales.g), su = scale_of_bits<KIND>(scales.u), su2 = scale_of_bits<KIND>(scales.u2);
+        scales = scales_of(item + step < item1 ? item + step : item);
+        StagedBlock<DT> raw;
+        const auto load_x = [&](int kb) {
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        bf16x8_t y[S][2];
-                        load_token<DT, S>(x, k + half * 64 + quad * 16, a.hidden, y);
-#pragma unroll
-                        for (int s = 0; s < S; ++s) {
-                            pg = add_products(half ? fg.b : fg.a, y[s], pg);
-                            pu = add_products(half ? fu.b : fu.a, y[s], pu);
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        ag[i] = fmaf(pg[i], sg, ag[i]);
-                        au[i] = fmaf(pu[i], i < in_first ? su : su2, au[i]);
-                    }
-                }
+            for (int i = 0; i < kLoads; ++i)
+                raw.v[i] = load_piece<DT>(mine_x[i], static_cast<int64_t>(kb) * kF8Block + (lane % kLanes) * Arith<DT>::kLanes, a.hidden);
+        };
+        const auto stage_x = [&] {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            stage_tokens<DT, S>(raw, staged[wave]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        };
+        if (r != r_now) {
+            const Chosen mine = find_tokens(a, routing, __builtin_amdgcn_readfirstlane(routing.reached[r]));
+            n = mine.n;
+            meet();  // the last expert's tables have been read
+            if (wave == 0 && mine.here) {
+                tokens[mine.rank] = lane;
+                slots[mine.rank] = mine.slot;
+                weights[mine.rank] = mine.weight;
             }
-            *reinterpret_cast<f32x4_t*>(&sums[wave][l16][quad * 4]) = ag;
-            *reinterpret_cast<f32x4_t*>(&sums[wave][l16][kTile + quad * 4]) = au;
-            __syncthreads();
-            if (tid < kTile * kTile) {
-                const int y = y0 + tid / kTile, c = tid % kTile;
-                if (y < n) {
-                    float g = 0.0f, u = 0.0f;
+            meet();
+            r_now = r;
+            if (n <= kStaged && kb0 < kb1) {
 #pragma unroll
-                    for (int w = 0; w < kWaves; ++w) {
-                        g += sums[w][tid / kTile][c];
-                        u += sums[w][tid / kTile][kTile + c];
-                    }
-                    const float v = c0 + c < a.inner ? weights[y] * (g * sigmoid(g) * u) : 0.0f;
-                    uint32_t part[HS];
-                    split<HS>(v, part);
-#pragma unroll
-                    for (int s = 0; s < HS; ++s)
-                        h[(static_cast<int64_t>(slots[y]) * HS + s) * width + c0 + c] = static_cast<uint16_t>(part[s]);
-                }
+                for (int i = 0; i < kLoads; ++i)
+                    mine_x[i] = static_cast<const char*>(a.x) + tokens[min(i * (64 / kLanes) + lane / kLanes, n - 1)] * a.x_stride * Arith<DT>::kEsize;
+                load_x(kb0);
+                stage_x();
             }
-            __syncthreads();
+        }
+        const int in_first = kF8Block - static_cast<int>((a.inner + c0) % kF8Block) - quad * 4;  // of this lane's up columns
+        f32x4_t ag[YT], au[YT];
+#pragma unroll
+        for (int t = 0; t < YT; ++t) ag[t] = au[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        RawFrag g, u;
+        const auto take = [&](Stage& s) {
+            g = turn(s.g, turning[wave][0]);
+            u = turn(s.u, turning[wave][1]);
+            load(s);
+        };
+        const auto products = [&](int kb, const Tokens<S>& y, int t) {
+            const f32x4_t pg = block_sum<S>(g, y), pu = block_sum<S>(u, y);
+            const float fg = lane_value(sg, kb - kb0), fu = lane_value(su, kb - kb0), fu2 = lane_value(su2, kb - kb0);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                ag[t][q] = fmaf(pg[q], fg, ag[t][q]);
+                au[t][q] = fmaf(pu[q], q < in_first ? fu : fu2, au[t][q]);
+            }
+        };
+        if (n <= kStaged) {
+            // While a block is multiplied the next one is loaded, behind the last the first again, for the next item.
+            in_turns(stages, turn_at, kb0, kb1, [&](Stage& s, int kb) {
+                const Tokens<S> y = staged_tokens<S>(staged[wave], min(l16, kStaged - 1));
+                load_x(kb + 1 < kb1 ? kb + 1 : kb0);
+                take(s);
+                products(kb, y, 0);
+                stage_x();
+            });
+        } else {
+            in_turns(stages, turn_at, kb0, kb1, [&](Stage& s, int kb) {
+                const int64_t k = static_cast<int64_t>(kb) * kF8Block + quad * 16;
+                const auto token = [&](int t) {
+                    return static_cast<const char*>(a.x) + tokens[min(t * kTile + l16, n - 1)] * a.x_stride * Arith<DT>::kEsize;
+                };
+                RawTokens<DT> raw = load_tokens<DT>(token(0), k, a.hidden);
+                take(s);
+#pragma unroll
+                for (int t = 0; t < YT; ++t) {
+                    if (t * kTile >= n) break;
+                    if (YT > 1) __builtin_amdgcn_sched_barrier(0);  // a tile's registers are the last one's
+                    if (t) raw = load_tokens<DT>(token(t), k, a.hidden);
+                    products(kb, to_parts<DT, S>(raw), t);
+                }
+            });
+        }
+#pragma unroll
+        for (int t = 0; t < YT; ++t) {
+            if (t * kTile >= n) break;
+            if (t || item > item0) meet();  // the last sums have been read
+            *reinterpret_cast<f32x4_t*>(&sums[wave][l16][quad * 4]) = ag[t];
+            *reinterpret_cast<f32x4_t*>(&sums[wave][l16][kTile + quad * 4]) = au[t];
+            meet();
+            for (int o = tid; o < min(n - t * kTile, kTile) * kTile; o += kWaves * 64) {
+                const int y = o / kTile, c = o % kTile;
+                float vg = 0.0f, vu = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    vg += sums[w][y][c];
+                    vu += sums[w][y][kTile + c];
+                }
+                const float v = c0 + c < a.inner ? weights[t * kTile + y] * (vg * sigmoid(vg) * vu) : 0.0f;
+                uint32_t part[HS];
+                split<HS>(v, part);
+#pragma unroll
+                for (int p = 0; p < HS; ++p)
+                    h[(static_cast<int64_t>(slots[t * kTile + y]) * HS + p) * width + c0 + c] = static_cast<uint16_t>(part[p]);
+            }
         }
     }
 }
 
-// out: work item 16 columns.  The reached experts' blocks of h follow each other in one line, of which every wave takes
-// a run; each wave keeps sums of its own for every token, and the waves' are added in order.
-template <int DT, int KIND>
-__global__ __launch_bounds__(kWaves * 64) void k_few_down(FewArgs a, const uint16_t* __restrict__ h) {
-    constexpr int HS = kHParts<DT>;
+// out: work item 16 XT columns.  The reached experts' blocks of h follow each other in one line, of which every wave takes
+// a run, its next blocks under way whichever experts they are of, and keeps sums of its own for every token; the
+// waves' are added in order.
+template <int DT, int KIND, int XT, int YT>
+__global__ __launch_bounds__(kWaves * 64, 2) void k_few_down(FewArgs a, const uint16_t* __restrict__ h) {
+    constexpr int HS = kHParts<DT>, kCols = XT * kTile;
     __shared__ Routing routing;
     __shared__ int tokens[kWaves][kFewTokens], slots[kWaves][kFewTokens];
-    __shared__ float sums[kWaves][kFewTokens][kTile];
+    __shared__ __align__(16) uint8_t turning[kWaves][kTile * kF8Block];
+    __shared__ __align__(16) uint8_t staged[kWaves][kStagedBytes<HS>];
+    extern __shared__ __align__(16) float sums[];  // [waves][tokens][columns]
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    float* const own = sums + wave * a.tokens * kCols;
     find_experts(a, routing);
     const int blocks = static_cast<int>(f8_width(a.inner) / kF8Block);
     const int64_t width = static_cast<int64_t>(blocks) * kF8Block;
     const int64_t pitch = (blocks + 3) / 4 * 4;
     const int64_t scale_rows = (a.hidden + kF8Block - 1) / kF8Block;
-    const int tiles = static_cast<int>((a.hidden + kTile - 1) / kTile);
+    const int tiles = static_cast<int>((a.hidden + kCols - 1) / kCols);
     const int units = routing.count * blocks;
-    const int per = (units + kWaves - 1) / kWaves;
-    const int u0 = min(wave * per, units), u1 = min(u0 + per, units);
+    const int u0 = static_cast<int>(static_cast<int64_t>(units) * wave / kWaves);
+    const int u1 = static_cast<int>(static_cast<int64_t>(units) * (wave + 1) / kWaves);
     constexpr int kSS = KIND == kScaleF32 ? 4 : 1;
     for (int item = blockIdx.x; item < tiles; item += gridDim.x) {
-        const int64_t c0 = static_cast<int64_t>(item) * kTile;
-        for (int i = lane; i < a.tokens * kTile; i += 64) (&sums[wave][0][0])[i] = 0.0f;
+        const int64_t c0 = static_cast<int64_t>(item) * kCols;
+        uint32_t row[2 * XT];  // this lane's parts of the rows, in a matrix of less than 2^32 bytes
+#pragma unroll
+        for (int x = 0; x < 2 * XT; ++x)
+            row[x] = static_cast<uint32_t>(min(c0 + x * 8 + (lane >> 3), a.hidden - 1) * width) + (lane & 7) * 16;
+        for (int i = lane; i < a.tokens * kCols; i += 64) own[i] = 0.0f;
+        struct Stage {
+            RawBlock w[XT];
+        };
+        // The next block to load, whichever expert it is of; past the run's end the last again.  (What is loaded in a branch,
+        // or copied before it is used, the compiler waits for at once.)
+        int left = u1 - u0, next_kb = units ? u0 % blocks : 0, next_r = units ? u0 / blocks : 0;
+        const auto matrix = [&](int r) {
+            return static_cast<const uint8_t*>(a.w2) + __builtin_amdgcn_readfirstlane(routing.reached[r]) * a.hidden * width;
+        };
+        const uint8_t* next_w2 = static_cast<const uint8_t*>(a.w2);
+        if (left > 0) next_w2 = matrix(next_r);
+        const auto load = [&](Stage& s) {
+            const uint8_t* const w2 = next_w2 + static_cast<int64_t>(next_kb) * kF8Block;
+#pragma unroll
+            for (int x = 0; x < XT; ++x) s.w[x] = load_block(w2 + row[2 * x], w2 + row[2 * x + 1]);
+            if (--left > 0 && ++next_kb == blocks) {
+                next_kb = 0;
+                next_w2 = matrix(++next_r);
+            }
+        };
+        Stage stages[2];
+        int turn_at = 0;  // the stage that the next block is in
+        if (u0 < u1) {
+            load(stages[0]);
+            load(stages[1]);
+        }
         for (int u = u0; u < u1;) {
-            const int from = u % blocks, to = min(blocks, from + (u1 - u));
-            const int e = routing.reached[u / blocks];
-            u += to - from;
+            const int from = u % blocks, to = min(min(blocks, from + 64), from + (u1 - u));
+            const int e = __builtin_amdgcn_readfirstlane(routing.reached[u / blocks]);
+            // The scales of these blocks, lane i that of the i-th.
+            const float scales = scale_of_bits<KIND>(scale_bits<KIND>(
+                static_cast<const uint8_t*>(a.w2_scale) + (e * scale_rows + c0 / kF8Block) * pitch * kSS, min(from + lane, blocks - 1)));
             const Chosen mine = find_tokens(a, routing, e);
             const int n = mine.n;
+            u += to - from;
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             if (mine.here) {
                 tokens[wave][mine.rank] = lane;
                 slots[wave][mine.rank] = mine.slot;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            const uint8_t* const w2 = static_cast<const uint8_t*>(a.w2) + (e * a.hidden + min(c0 + l16, a.hidden - 1)) * width + quad * 16;
-            const uint8_t* const ws = static_cast<const uint8_t*>(a.w2_scale) + (e * scale_rows + c0 / kF8Block) * pitch * kSS;
-            for (int y0 = 0; y0 < n; y0 += kTile) {
-                const int y = min(y0 + l16, n - 1);
-                const uint16_t* const row = h + static_cast<int64_t>(slots[wave][y]) * HS * width + quad * 16;
-                f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-                for (int kb = from; kb < to; ++kb) {
-                    const int64_t k = static_cast<int64_t>(kb) * kF8Block;
-                    const RawFrag f = load_frag(w2 + k);
-                    const float sc = scale_value<KIND>(ws, kb);
-                    f32x4_t p = {0.0f, 0.0f, 0.0f, 0.0f};
+            const uint16_t* from_h[YT];
+            f32x4_t acc[YT][XT];
 #pragma unroll
-                    for (int half = 0; half < 2; ++half)
+            for (int t = 0; t < YT; ++t) {
+                from_h[t] = h + static_cast<int64_t>(slots[wave][min(t * kTile + l16, n - 1)]) * HS * width + quad * 16;
 #pragma unroll
-                        for (int s = 0; s < HS; ++s) {
-                            const uint4* const at = reinterpret_cast<const uint4*>(row + s * width + k + half * 64);
-                            const bf16x8_t v[2] = {__builtin_bit_cast(bf16x8_t, at[0]), __builtin_bit_cast(bf16x8_t, at[1])};
-                            p = add_products(half ? f.b : f.a, v, p);
-                        }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[i] = fmaf(p[i], sc, acc[i]);
-                }
-                if (y0 + l16 < n) {
-                    f32x4_t* const at = reinterpret_cast<f32x4_t*>(&sums[wave][tokens[wave][y]][quad * 4]);
-                    *at = *at + acc;
-                }
+                for (int x = 0; x < XT; ++x) acc[t][x] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
             }
+            const auto load_h16 = [&](int t, int kb) {
+                Tokens<HS> v;
+#pragma unroll
+                for (int p = 0; p < HS; ++p)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint4* const at = reinterpret_cast<const uint4*>(from_h[t] + p * width + kb * kF8Block + half * 64);
+                        v.v[p][half][0] = __builtin_bit_cast(bf16x8_t, at[0]);
+                        v.v[p][half][1] = __builtin_bit_cast(bf16x8_t, at[1]);
+                    }
+                return v;
+            };
+            RawFrag w[XT];
+            const auto take = [&](Stage& s) {
+#pragma unroll
+                for (int x = 0; x < XT; ++x) w[x] = turn(s.w[x], turning[wave]);
+                load(s);
+            };
+            const auto products = [&](int kb, const Tokens<HS>& v, int t) {
+                const float scale = lane_value(scales, kb - from);
+#pragma unroll
+                for (int x = 0; x < XT; ++x) {
+                    const f32x4_t p = block_sum<HS>(w[x], v);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[t][x][q] = fmaf(p[q], scale, acc[t][x][q]);
+                }
+            };
+            if (n <= kStaged) {
+                // 16 lanes read a part of a row.
+                const uint16_t* mine_h[HS];
+                int at[HS];
+#pragma unroll
+                for (int i = 0; i < HS; ++i) {
+                    const int piece = i * 4 + (lane >> 4), y = piece / HS;
+                    mine_h[i] = h + (static_cast<int64_t>(slots[wave][min(y, n - 1)]) * HS + piece % HS) * width + (lane & 15) * 8;
+                    at[i] = piece * 2 * kF8Block + (((lane & 15) ^ y) * 16);
+                }
+                struct {
+                    u32x4_t v[HS];
+                } raw;
+                const auto load_h = [&](int kb) {
+#pragma unroll
+                    for (int i = 0; i < HS; ++i) raw.v[i] = *reinterpret_cast<const u32x4_t*>(mine_h[i] + min(kb, to - 1) * kF8Block);
+                };
+                const auto stage_h = [&] {
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+                    for (int i = 0; i < HS; ++i) *reinterpret_cast<u32x4_t*>(staged[wave] + at[i]) = raw.v[i];
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                };
+                load_h(from);
+                stage_h();
+                in_turns(stages, turn_at, from, to, [&](Stage& s, int kb) {
+                    const Tokens<HS> v = staged_tokens<HS>(staged[wave], min(l16, kStaged - 1));
+                    load_h(kb + 1);
+                    take(s);
+                    products(kb, v, 0);
+                    stage_h();
+                });
+            } else {
+                in_turns(stages, turn_at, from, to, [&](Stage& s, int kb) {
+                    Tokens<HS> v = load_h16(0, kb);
+                    take(s);
+#pragma unroll
+                    for (int t = 0; t < YT; ++t) {
+                        if (t * kTile >= n) break;
+                        if (YT > 1) __builtin_amdgcn_sched_barrier(0);  // a tile's registers are the last one's
+                        if (t) v = load_h16(t, kb);
+                        products(kb, v, t);
+                    }
+                });
+            }
+#pragma unroll
+            for (int t = 0; t < YT; ++t)
+                if (t * kTile + l16 < n) {
+#pragma unroll
+                    for (int x = 0; x < XT; ++x) {
+                        f32x4_t* const at = reinterpret_cast<f32x4_t*>(own + tokens[wave][t * kTile + l16] * kCols + x * kTile + quad * 4);
+                        *at = *at + acc[t][x];
+                    }
+                }
         }
-        __syncthreads();
-        for (int i = tid; i < a.tokens * kTile; i += kWaves * 64) {
-            const int t = i / kTile, c = i % kTile;
+        meet();
+        const int outputs = a.tokens * kCols;
+        for (int i = tid; i < outputs; i += kWaves * 64) {
             float v = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) v += sums[w][t][c];
-            if (c0 + c < a.hidden) Arith<DT>::store1(a.out, t * a.hidden + c0 + c, v);
+            for (int w = 0; w < kWaves; ++w) v += sums[w * outputs + i];
+            const int64_t t = i / kCols, c = c0 + i % kCols;
+            if (c < a.hidden) Arith<DT>::store1(a.out, t * a.hidden + c, v);
         }
-        __syncthreads();
+        meet();
     }
 }
 
@@ -367,26 +719,41 @@ size_t expert_layer_few_workspace(int tokens, int topk, int64_t hidden, int64_t 
 hipError_t launch_expert_layer_few(const FewArgs& a, hipStream_t stream) {
     uint16_t* const h = static_cast<uint16_t*>(a.workspace);
     const int64_t experts = std::min<int64_t>(static_cast<int64_t>(a.tokens) * a.topk, a.experts);
-    const int64_t up = std::min<int64_t>(experts * (f8_width(a.inner) / kTile), grid_limit(int64_t(1) << 20));
-    const int64_t down = std::min<int64_t>((a.hidden + kTile - 1) / kTile, grid_limit(int64_t(1) << 20));
-    const auto run = [&](auto dt, auto kind) {
-        constexpr int DT = decltype(dt)::value, KIND = decltype(kind)::value;
-        k_few_up<DT, KIND><<<static_cast<uint32_t>(up), kWaves * 64, 0, stream>>>(a, h);
-        k_few_down<DT, KIND><<<static_cast<uint32_t>(down), kWaves * 64, 0, stream>>>(a, h);
+    // A workgroup for each compute unit (two of them hold the registers of no more).
+    const int64_t up = std::min(std::min<int64_t>(experts * (f8_width(a.inner) / kTile), 256), grid_limit(256));
+    // 32 columns an item read h half as often as 16 (1 token, hidden 7168: 25 us, with 16 columns 33), but leave compute
+    // units without work where there are fewer than about 200 (7 tokens, hidden 2880, fp32: the layer 88 us, with 16 82).
+    const auto items = [&](int xt) { return (a.hidden + xt * kTile - 1) / (xt * kTile); };
+    const int xt = a.tokens <= kTile && items(2) < 192 ? 1 : 2;
+    const int64_t down = std::min<int64_t>(items(xt), grid_limit(int64_t(1) << 20));
+    const size_t lds = static_cast<size_t>(kWaves) * a.tokens * xt * kTile * sizeof(float);
+    using std::integral_constant;
+    const auto run = [&](auto dt, auto kind, auto yt) {
+        constexpr int DT = decltype(dt)::value, KIND = decltype(kind)::value, YT = decltype(yt)::value;
+        k_few_up<DT, KIND, YT><<<static_cast<uint32_t>(up), kWaves * 64, 0, stream>>>(a, h);
+        note_launch("k_few_up", kMapLinear, 1, up, kWaves * 64, 1);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        if constexpr (YT == 1) {
+            if (xt == 1) {
+                k_few_down<DT, KIND, 1, YT><<<static_cast<uint32_t>(down), kWaves * 64, lds, stream>>>(a, h);
+                note_launch("k_few_down", kMapLinear, 1, down, kWaves * 64, 1);
+                return hipGetLastError();
+            }
+        }
+        k_few_down<DT, KIND, 2, YT><<<static_cast<uint32_t>(down), kWaves * 64, lds, stream>>>(a, h);
+        note_launch("k_few_down", kMapLinear, 1, down, kWaves * 64, 2);
+        return hipGetLastError();
+    };
+    const auto sized = [&](auto dt, auto kind) {
+        if (a.tokens <= kTile) return run(dt, kind, integral_constant<int, 1>{});
+        return run(dt, kind, integral_constant<int, kFewTokens / kTile>{});
     };
     const auto typed = [&](auto dt) {
-        if (a.kind == kScaleF32)
-            run(dt, std::integral_constant<int, kScaleF32>{});
-        else
-            run(dt, std::integral_constant<int, kScaleE8m0>{});
+        if (a.kind == kScaleF32) return sized(dt, integral_constant<int, kScaleF32>{});
+        return sized(dt, integral_constant<int, kScaleE8m0>{});
     };
-    if (a.dtype == kDtF32)
-        typed(std::integral_constant<int, kDtF32>{});
-    else
-        typed(std::integral_constant<int, kDtBf16>{});
-    note_launch("k_few_up", kMapLinear, 1, up, kWaves * 64, 1);
-    note_launch("k_few_down", kMapLinear, 1, down, kWaves * 64, 1);
-    return hipGetLastError();
+    if (a.dtype == kDtF32) return typed(integral_constant<int, kDtF32>{});
+    return typed(integral_constant<int, kDtBf16>{});
 }
 
 }  // namespace nuna

@@ -467,6 +467,23 @@ def test_few(nuna, T, k, E, first, count, H, inner, dtype, kind):
     assert torch.equal(nuna.expert_layer_few(x, dev(idx), w, *packed, first_expert=first), out)
 
 
+@pytest.mark.parametrize("H,inner,cap", [(128, 640, 3), (200, 200, 1), (1152, 256, 2), (2200, 128, 1), (640, 384, 5)])
+def test_few_workgroups_of_many_items(nuna, H, inner, cap):
+    """Few workgroups, whose waves have one to three blocks of an item and load those of the next ones ahead."""
+    idx = routing(21, 3, 7, H)
+    packed, plain = experts_of(nuna, 7, H, inner, "f32", H)
+    x, x64 = values((21, H), "bf16", 5, 0.3)
+    w = torch.rand((21, 3), generator=torch.Generator().manual_seed(1)).cuda()
+    want = nuna.expert_layer_few(x, dev(idx), w, *packed)
+    try:
+        assert nuna.lib().nuna_set_max_workgroups(cap) == 0
+        got = check_few(nuna, x, x64, idx, w, packed, plain, 0, "bf16")
+        few = nuna.expert_layer_few(x[:9], dev(idx[:9]), w[:9], *packed)
+    finally:
+        nuna.lib().nuna_set_max_workgroups(0)
+    assert torch.equal(got, want) and torch.equal(few, nuna.expert_layer_few(x[:9], dev(idx[:9]), w[:9], *packed))
+
+
 def test_few_tables_of_any_numbers(nuna):
     """The same expert twice, all tokens at one expert, none here, and numbers at the ends of int32."""
     packed, plain = experts_of(nuna, 4, 128, 128, "e8m0", 1)
