@@ -621,7 +621,7 @@ nuna_status_t nuna_f8_wgrad(const void* a, const void* a_scale, const void* b, c
  *   dout, dx  [rows][cols] of dtype;  z [rows][z_stride >= cols], as it was normed
  *   workspace nuna_rms_norm_grad_workspace bytes, 16-byte aligned
  */
-#define NUNA_NORM_MAX_COLS 32768
+#define NUNA_NORM_MAX_COLS 16384
 nuna_status_t nuna_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
                             const void* weight, nuna_dtype_t weight_dtype, float eps, size_t rows, size_t cols, void* sum,
                             int64_t sum_stride, void* out, void* q, void* q_scale, nuna_scale_t kind, float* rstd,

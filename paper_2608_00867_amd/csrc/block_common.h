@@ -25,19 +25,64 @@ __device__ __forceinline__ void load8(const char* p, int64_t n, float (&v)[8]) {
     }
 }
 
-// The first `n` of eight values, rounded to the type.
-template <int DT>
+// The first `n` of eight values, rounded to the type.  NT: streamed past the caches' other contents.
+template <int DT, bool NT = false>
 __device__ __forceinline__ void store8(char* p, int64_t n, const float (&v)[8]) {
     constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
     if (n >= 8) {
 #pragma unroll
         for (int i = 0; i < 8 / L; ++i)
-            store16_any<false>(p + i * 16, Arith<DT>::narrow(reinterpret_cast<const float(&)[L]>(v[i * L])));
+            store16_any<NT>(p + i * 16, Arith<DT>::narrow(reinterpret_cast<const float(&)[L]>(v[i * L])));
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < n) Arith<DT>::store1(p + i * ES, 0, v[i]);
     }
+}
+
+// Eight values as they are stored.
+template <int DT>
+struct Raw8 {
+    u32x4_t v[8 / Arith<DT>::kLanes];
+};
+// Eight values from column c of a row of `cols` on; zeros from the row's end on.  WHOLE: the row is a multiple of eight, and
+// the load is made whatever c is (of the last eight): what is loaded in a branch the compiler waits for together with all
+// that was loaded after it.  What lies past the end then has to be put out by `widen`.
+template <int DT, bool WHOLE>
+__device__ __forceinline__ Raw8<DT> load_raw8(const char* row, int64_t c, int64_t cols) {
+    constexpr int ES = Arith<DT>::kEsize, L = Arith<DT>::kLanes;
+    Raw8<DT> r;
+    if constexpr (WHOLE) {
+        const char* const p = row + min(c, cols - 8) * ES;
+#pragma unroll
+        for (int i = 0; i < 8 / L; ++i) r.v[i] = *reinterpret_cast<const u32x4_any_t*>(p + i * 16);
+    } else {
+        float v[8];
+        load8<DT>(row + c * ES, cols - c, v);
+#pragma unroll
+        for (int i = 0; i < 8 / L; ++i)
+            r.v[i] = __builtin_bit_cast(u32x4_t, Arith<DT>::narrow(reinterpret_cast<const float(&)[L]>(v[i * L])));
+    }
+    return r;
+}
+// Their values; zeros where they do not exist.
+template <int DT>
+__device__ __forceinline__ void widen(const Raw8<DT>& r, bool exist, float (&v)[8]) {
+    constexpr int L = Arith<DT>::kLanes;
+#pragma unroll
+    for (int i = 0; i < 8 / L; ++i) {
+        const u32x4_t u = exist ? r.v[i] : u32x4_t{0, 0, 0, 0};
+        Arith<DT>::init(reinterpret_cast<float(&)[L]>(v[i * L]), __builtin_bit_cast(uint4, u));
+    }
+}
+
+// The same; `streamed`: what is written does not fit the L2s, so none of it will be found there.
+template <int DT>
+__device__ __forceinline__ void store8(char* p, int64_t n, const float (&v)[8], bool streamed) {
+    if (streamed)
+        store8<DT, true>(p, n, v);
+    else
+        store8<DT, false>(p, n, v);
 }
 
 // Values as they are after rounding to the type.
@@ -75,15 +120,18 @@ __device__ __forceinline__ float sum_lanes(float v) {
     return a + b;
 }
 
-// 1 / (1 + exp(-g)), within 3 units of fp32's last place from -87 up, 0 below (where it is under 2^-125).  The exponent
-// is kept in two parts, so that its rounding does not grow with g.
+// 1 / (1 + exp(-g)), about as exact as with the library's exponential and a division, at a third of their instructions; 0
+// below -87 (where it is under 2^-125).  The exponent is kept in two parts, so that its rounding does not grow with g, and
+// the reciprocal is improved once.
 __device__ __forceinline__ float sigmoid(float g) {
     const float x = -__builtin_amdgcn_fmed3f(g, -87.0f, 87.0f);
     const float hi = x * 1.44269502f;  // log2(e) = 1.44269502 + 1.9259630e-8
     const float lo = fmaf(x, 1.9259630e-8f, fmaf(x, 1.44269502f, -hi));
     float e = __builtin_amdgcn_exp2f(hi);
     e = fmaf(e, lo * 0.693147182f, e);
-    const float s = __builtin_amdgcn_rcpf(1.0f + e);
+    const float d = 1.0f + e;
+    float s = __builtin_amdgcn_rcpf(d);
+    s = fmaf(fmaf(-d, s, 1.0f), s, s);
     return g < -87.0f ? 0.0f : s;
 }
 

@@ -61,6 +61,10 @@ nuna_status_t check_swiglu(const void* dout, const void* gu, const int32_t* offs
          {"q_scale", q_scale, q ? product(rows, f8_pitch(cols), 1, f8_scale_size(kind)) : 0, 16, true}});
 }
 
+bool swiglu_streamed(size_t values, const void* out, const void* q, int dtype) {
+    return streamed(static_cast<int64_t>(values * ((out ? dtype_size(dtype) : 0) + (q ? 1 : 0))));
+}
+
 }  // namespace
 
 extern "C" {
@@ -99,7 +103,8 @@ nuna_status_t nuna_rms_norm(const void* x, int64_t x_stride, const void* residua
                             {"rstd", rstd, rstd ? 4 * rows : 0, 4, true}}));
     if (rows == 0) return api_ok();
     const NormArgs a = {x, x_stride, residual, residual_stride, weight, weight_dtype, eps, static_cast<int64_t>(rows),
-                        static_cast<int64_t>(cols), sum, sum_stride, out, q, q_scale, kind, rstd, dtype};
+                        static_cast<int64_t>(cols), sum, sum_stride, out, q, q_scale, kind, rstd, dtype,
+                        streamed(static_cast<int64_t>(rows * cols) * ((residual ? es : 0) + (out ? es : 0) + (q ? 1 : 0)))};
     return api_hip(launch_rms_norm(a, stream), "norm launch");
 } catch (...) {
     return api_exception();
@@ -132,7 +137,7 @@ nuna_status_t nuna_rms_norm_grad(const void* dout, const void* z, int64_t z_stri
                             {"dweight", dweight, 4 * cols, 16, true},
                             {"workspace", workspace, need, 16, true}}));
     const NormGradArgs a = {dout, z, z_stride, weight, weight_dtype, rstd, dsum, static_cast<int64_t>(rows),
-                            static_cast<int64_t>(cols), dx, dweight, workspace, dtype};
+                            static_cast<int64_t>(cols), dx, dweight, workspace, dtype, streamed(static_cast<int64_t>(each))};
     return api_hip(launch_rms_norm_grad(a, stream), "norm gradient launch");
 } catch (...) {
     return api_exception();
@@ -181,7 +186,7 @@ nuna_status_t nuna_swiglu(const void* gu, const int32_t* offsets, int groups, si
     NUNA_TRY(check_swiglu(nullptr, gu, offsets, groups, rows, inner, inner, out, q, q_scale, kind, dtype));
     if (rows == 0) return api_ok();
     const SwigluArgs a = {nullptr, gu, offsets, groups, static_cast<int64_t>(rows), static_cast<int64_t>(inner), out, q,
-                          q_scale, kind, dtype};
+                          q_scale, kind, dtype, swiglu_streamed(rows * inner, out, q, dtype)};
     return api_hip(launch_swiglu(a, stream), "SwiGLU launch");
 } catch (...) {
     return api_exception();
@@ -195,7 +200,7 @@ nuna_status_t nuna_swiglu_grad(const void* dout, const void* gu, const int32_t* 
     NUNA_TRY(check_swiglu(dout, gu, offsets, groups, rows, inner, 2 * inner, out, q, q_scale, kind, dtype));
     if (rows == 0) return api_ok();
     const SwigluArgs a = {dout, gu, offsets, groups, static_cast<int64_t>(rows), static_cast<int64_t>(inner), out, q,
-                          q_scale, kind, dtype};
+                          q_scale, kind, dtype, swiglu_streamed(2 * rows * inner, out, q, dtype)};
     return api_hip(launch_swiglu_grad(a, stream), "SwiGLU gradient launch");
 } catch (...) {
     return api_exception();

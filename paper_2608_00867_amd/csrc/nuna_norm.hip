@@ -20,6 +20,11 @@ namespace {
 
 constexpr int kNone = -1;
 
+// Of rows of one chunk a thread the next one is loaded while this one is summed, and the weights are kept; wider ones do
+// not leave the registers for it.
+template <int NV>
+constexpr bool kAhead = NV == 1;
+
 // Eight weights, of the rows' type or fp32.
 template <int DT>
 __device__ __forceinline__ void load_weights(const void* w, bool w32, int64_t c, int64_t n, float (&v)[8]) {
@@ -29,8 +34,9 @@ __device__ __forceinline__ void load_weights(const void* w, bool w32, int64_t c,
         load8<DT>(static_cast<const char*>(w) + c * Arith<DT>::kEsize, n, v);
 }
 
-// P lanes a row, 256 threads a workgroup, or (P = 0) a workgroup a row; NV chunks of eight values a thread.
-template <int DT, int KIND, int NV, int P>
+// P lanes a row, 256 threads a workgroup, or (P = 0) a workgroup a row; NV chunks of eight values a thread.  A workgroup
+// takes rows in turn and loads the next one before it sums this one.
+template <int DT, int KIND, int NV, int P, bool WHOLE>
 __global__ __launch_bounds__(P ? kWG : 1024) void k_rms_norm(NormArgs a) {
     constexpr int ES = Arith<DT>::kEsize;
     constexpr int kRows = P ? kWG / P : 1;
@@ -38,58 +44,81 @@ __global__ __launch_bounds__(P ? kWG : 1024) void k_rms_norm(NormArgs a) {
     const int width = P ? P : blockDim.x;
     const int t = P ? threadIdx.x % P : threadIdx.x;
     const int64_t blocks = (a.cols + kF8Block - 1) / kF8Block, pitch = (blocks + 3) / 4 * 4;
+    const auto column = [&](int i) { return (static_cast<int64_t>(i) * width + t) * 8; };
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kRows + (P ? threadIdx.x / P : 0);
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+    // Without a residual x stands in for it, whose values are not used.
+    const void* const residual = a.residual ? a.residual : a.x;
+    const int64_t residual_stride = a.residual ? a.residual_stride : a.x_stride;
+    Raw8<DT> x[NV], r[NV];
+    const auto load = [&](int64_t row) {
+        row = min(row, a.rows - 1);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            x[i] = load_raw8<DT, WHOLE>(static_cast<const char*>(a.x) + row * a.x_stride * ES, column(i), a.cols);
+            r[i] = load_raw8<DT, WHOLE>(static_cast<const char*>(residual) + row * residual_stride * ES, column(i), a.cols);
+        }
+    };
+    float w[NV][8];
+    const auto load_w = [&](int i) { load_weights<DT>(a.weight, a.weight_dtype == kDtF32, column(i), a.cols - column(i), w[i]); };
+    if constexpr (kAhead<NV>) {
+        load(first);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) load_w(i);
+    }
     int turn = 0;
-    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < a.rows; row0 += static_cast<int64_t>(gridDim.x) * kRows) {
+    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < a.rows; row0 += step) {
         const int64_t row = row0 + (P ? threadIdx.x / P : 0);
         const int64_t cols = row < a.rows ? a.cols : 0;  // a row past the last has no values
+        if constexpr (!kAhead<NV>) load(row);
         float z[NV][8];
         float squares = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int64_t c = (static_cast<int64_t>(i) * width + t) * 8;
-            load8<DT>(static_cast<const char*>(a.x) + (row * a.x_stride + c) * ES, cols - c, z[i]);
-        }
-        if (a.residual) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int64_t c = (static_cast<int64_t>(i) * width + t) * 8;
+            const int64_t c = column(i);
+            widen<DT>(x[i], c < cols, z[i]);
+            if (a.residual) {
                 float v[8];
-                load8<DT>(static_cast<const char*>(a.residual) + (row * a.residual_stride + c) * ES, cols - c, v);
+                widen<DT>(r[i], c < cols, v);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) z[i][j] += v[j];
                 round8<DT>(z[i]);
-                store8<DT>(static_cast<char*>(a.sum) + (row * a.sum_stride + c) * ES, cols - c, z[i]);
             }
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) squares = fmaf(z[i][j], z[i][j], squares);
+        }
+        // The sum may lie over x or the residual: of its own row, which has been read.
+        if (kAhead<NV> && row0 + step < a.rows) load(row + step);
+        if (a.residual) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                store8<DT>(static_cast<char*>(a.sum) + (row * a.sum_stride + column(i)) * ES, cols - column(i), z[i], a.streamed);
+        }
         squares = P ? sum_lanes<P ? P : 64>(squares) : sum_workgroup(squares, parts[turn]);
         turn ^= 1;
-        const float r = 1.0f / sqrtf(squares / static_cast<float>(a.cols) + a.eps);
-        if (a.rstd && t == 0 && cols) a.rstd[row] = r;
+        const float rs = 1.0f / sqrtf(squares / static_cast<float>(a.cols) + a.eps);
+        if (a.rstd && t == 0 && cols) a.rstd[row] = rs;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int64_t c = (static_cast<int64_t>(i) * width + t) * 8;
-            float w[8];
-            load_weights<DT>(a.weight, a.weight_dtype == kDtF32, c, cols - c, w);
+            const int64_t c = column(i);
+            if constexpr (!kAhead<NV>) load_w(i);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) z[i][j] = z[i][j] * r * w[j];
-            if (a.out) store8<DT>(static_cast<char*>(a.out) + (row * a.cols + c) * ES, cols - c, z[i]);
+            for (int j = 0; j < 8; ++j) z[i][j] = z[i][j] * rs * w[i][j];
+            if (a.out) store8<DT>(static_cast<char*>(a.out) + (row * a.cols + c) * ES, cols - c, z[i], a.streamed);
             if constexpr (KIND != kNone) {
+                const int n = static_cast<int>(min(cols - c, static_cast<int64_t>(8)));
                 uint32_t m = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) m = max(m, c + j < cols ? abs_bits(z[i][j]) : 0);
+                for (int j = 0; j < 8; ++j) {
+                    z[i][j] = j < n ? z[i][j] : 0.0f;  // 0 times what need not be finite, past the row's end
+                    m = max(m, abs_bits(z[i][j]));
+                }
                 const BlockScale s = block_scale<KIND>(max16(m));
                 const int64_t block = c / kF8Block;
                 if (cols && block < blocks) {
                     uint2 q;
-                    float v[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? z[i][j] : 0.0f;
-                    q.x = to_e4m3x4(v[0] * s.r, v[1] * s.r, v[2] * s.r, v[3] * s.r);
-                    q.y = to_e4m3x4(v[4] * s.r, v[5] * s.r, v[6] * s.r, v[7] * s.r);
+                    q.x = to_e4m3x4(z[i][0] * s.r, z[i][1] * s.r, z[i][2] * s.r, z[i][3] * s.r);
+                    q.y = to_e4m3x4(z[i][4] * s.r, z[i][5] * s.r, z[i][6] * s.r, z[i][7] * s.r);
                     *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.q) + row * blocks * kF8Block + c) = q;
                     if (t % 16 == 0) store_scale<KIND>(a.q_scale, row * pitch + block, s.kept);
                 }
@@ -102,53 +131,68 @@ __global__ __launch_bounds__(P ? kWG : 1024) void k_rms_norm(NormArgs a) {
 
 // The same threads.  Part p of `parts` takes every parts-th set of rows and leaves its share of dw in row p of `partial`
 // [parts][cols]; parts do not depend on the number of workgroups, so neither does dw.
-template <int DT, int NV, int P>
-__global__ __launch_bounds__(P ? kWG : 1024) void k_rms_norm_grad(NormGradArgs a, float* __restrict__ partial, int64_t parts) {
+template <int DT, int NV, int P, bool WHOLE>
+__global__ __launch_bounds__(P ? kWG : 1024, P ? 1 : NV == 1 && DT == kDtBf16 ? 7 : 4) void k_rms_norm_grad(NormGradArgs a, float* __restrict__ partial, int64_t parts) {
     constexpr int ES = Arith<DT>::kEsize;
     constexpr int kRows = P ? kWG / P : 1;
     __shared__ float waves[2][16];
     __shared__ float sums[P ? kWG * 8 * NV : 1];
     const int width = P ? P : blockDim.x;
     const int t = P ? threadIdx.x % P : threadIdx.x;
+    const auto column = [&](int i) { return (static_cast<int64_t>(i) * width + t) * 8; };
+    // Without another gradient dout stands in for it, whose values are not used.
+    const void* const dsum = a.dsum ? a.dsum : a.dout;
+    Raw8<DT> z[NV], g[NV], d[NV];
+    float r_next = 0.0f;
+    const auto load = [&](int64_t row) {
+        row = min(row, a.rows - 1);
+        r_next = a.rstd[row];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            z[i] = load_raw8<DT, WHOLE>(static_cast<const char*>(a.z) + row * a.z_stride * ES, column(i), a.cols);
+            g[i] = load_raw8<DT, WHOLE>(static_cast<const char*>(a.dout) + row * a.cols * ES, column(i), a.cols);
+            d[i] = load_raw8<DT, WHOLE>(static_cast<const char*>(dsum) + row * a.cols * ES, column(i), a.cols);
+        }
+    };
+    float w[NV][8];
+    const auto load_w = [&](int i) { load_weights<DT>(a.weight, a.weight_dtype == kDtF32, column(i), a.cols - column(i), w[i]); };
     int turn = 0;
     for (int64_t part = blockIdx.x; part < parts; part += gridDim.x) {
         float dw[NV][8] = {};
+        const int64_t slot = P ? threadIdx.x / P : 0;
+        if constexpr (kAhead<NV>) load(part * kRows + slot);
         for (int64_t row0 = part * kRows; row0 < a.rows; row0 += parts * kRows) {
-            const int64_t row = row0 + (P ? threadIdx.x / P : 0);
+            const int64_t row = row0 + slot;
             const int64_t cols = row < a.rows ? a.cols : 0;
-            const float r = cols ? a.rstd[row] : 0.0f;
-            float zhat[NV][8], u[NV][8];
+            if constexpr (!kAhead<NV>) load(row);
+            const float r = r_next;
+            float zr[NV][8], u[NV][8], v[NV][8];
             float dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int64_t c = (static_cast<int64_t>(i) * width + t) * 8;
-                load8<DT>(static_cast<const char*>(a.z) + (row * a.z_stride + c) * ES, cols - c, zhat[i]);
-                load8<DT>(static_cast<const char*>(a.dout) + (row * a.cols + c) * ES, cols - c, u[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int64_t c = (static_cast<int64_t>(i) * width + t) * 8;
-                float w[8];
-                load_weights<DT>(a.weight, a.weight_dtype == kDtF32, c, cols - c, w);
+                widen<DT>(z[i], column(i) < cols, zr[i]);
+                widen<DT>(g[i], column(i) < cols, u[i]);
+                if constexpr (kAhead<NV>) widen<DT>(d[i], column(i) < cols && a.dsum, v[i]);
+                load_w(i);  // (kept, they would cost the second workgroup of a compute unit)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    zhat[i][j] *= r;
-                    dw[i][j] = fmaf(u[i][j], zhat[i][j], dw[i][j]);
-                    u[i][j] *= w[j];
-                    dot = fmaf(u[i][j], zhat[i][j], dot);
+                    zr[i][j] *= r;
+                    dw[i][j] = fmaf(u[i][j], zr[i][j], dw[i][j]);
+                    u[i][j] *= w[i][j];
+                    dot = fmaf(u[i][j], zr[i][j], dot);
                 }
             }
+            // dx may lie over dsum: of its own row, which has been read.
+            if (kAhead<NV> && row0 + parts * kRows < a.rows) load(row + parts * kRows);
             dot = P ? sum_lanes<P ? P : 64>(dot) : sum_workgroup(dot, waves[turn]);
             turn ^= 1;
             const float mean = dot / static_cast<float>(a.cols);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int64_t c = (static_cast<int64_t>(i) * width + t) * 8;
-                float v[8] = {};
-                if (a.dsum) load8<DT>(static_cast<const char*>(a.dsum) + (row * a.cols + c) * ES, cols - c, v);
+                if constexpr (!kAhead<NV>) widen<DT>(d[i], column(i) < cols && a.dsum, v[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = fmaf(r, u[i][j] - zhat[i][j] * mean, v[j]);
-                store8<DT>(static_cast<char*>(a.dx) + (row * a.cols + c) * ES, cols - c, v);
+                for (int j = 0; j < 8; ++j) v[i][j] = fmaf(r, u[i][j] - zr[i][j] * mean, v[i][j]);
+                store8<DT>(static_cast<char*>(a.dx) + (row * a.cols + column(i)) * ES, cols - column(i), v[i], a.streamed);
             }
         }
         float* const to = partial + part * a.cols;
@@ -203,6 +247,8 @@ __global__ __launch_bounds__(kDwWaves * 64) void k_rms_norm_dw(const float* __re
     }
 }
 
+constexpr int kNormWaves = 32;  // that a compute unit holds at most
+
 // f(chunks a thread, lanes a row, threads of a workgroup), the first two as types: few columns in parts of a wave,
 // others in a workgroup a row.
 template <class F>
@@ -219,10 +265,8 @@ void by_columns(int64_t cols, F f) {
         f(integral_constant<int, 2>{}, integral_constant<int, 64>{}, kWG);
     else if (cols <= 8192)
         f(integral_constant<int, 1>{}, integral_constant<int, 0>{}, threads(1));
-    else if (cols <= 16384)
-        f(integral_constant<int, 2>{}, integral_constant<int, 0>{}, threads(2));
     else
-        f(integral_constant<int, 4>{}, integral_constant<int, 0>{}, threads(4));
+        f(integral_constant<int, 2>{}, integral_constant<int, 0>{}, threads(2));
 }
 
 }  // namespace
@@ -231,10 +275,14 @@ hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream) {
     by_columns(a.cols, [&](auto nv, auto p, int threads) {
         constexpr int NV = decltype(nv)::value, P = decltype(p)::value;
         const int64_t sets = P ? (a.rows + kWG / (P ? P : 1) - 1) / (kWG / (P ? P : 1)) : a.rows;
-        const int64_t grid = std::min<int64_t>(sets, grid_limit(int64_t(1) << 20));
+        const int64_t grid = std::min<int64_t>(sets, grid_limit(int64_t(256) * (kNormWaves * 64 / threads)));
         const auto run = [&](auto dt, auto kind) {
-            k_rms_norm<decltype(dt)::value, decltype(kind)::value, NV, P>
-                <<<static_cast<uint32_t>(grid), threads, 0, stream>>>(a);
+            if (a.cols % 8 == 0)
+                k_rms_norm<decltype(dt)::value, decltype(kind)::value, NV, P, true>
+                    <<<static_cast<uint32_t>(grid), threads, 0, stream>>>(a);
+            else
+                k_rms_norm<decltype(dt)::value, decltype(kind)::value, NV, P, false>
+                    <<<static_cast<uint32_t>(grid), threads, 0, stream>>>(a);
         };
         const auto typed = [&](auto dt) {
             if (!a.q)
@@ -262,10 +310,20 @@ hipError_t launch_rms_norm_grad(const NormGradArgs& a, hipStream_t stream) {
             const int64_t sets = P ? (a.rows + kWG / (P ? P : 1) - 1) / (kWG / (P ? P : 1)) : a.rows;
             parts = std::min<int64_t>(sets, kNormGradParts);
             const int64_t grid = std::min(parts, grid_limit(parts));
+            const auto run = [&](auto dt, auto whole) {
+                k_rms_norm_grad<decltype(dt)::value, NV, P, decltype(whole)::value>
+                    <<<static_cast<uint32_t>(grid), threads, 0, stream>>>(a, partial, parts);
+            };
+            const auto typed = [&](auto dt) {
+                if (a.cols % 8 == 0)
+                    run(dt, std::true_type{});
+                else
+                    run(dt, std::false_type{});
+            };
             if (a.dtype == kDtF32)
-                k_rms_norm_grad<kDtF32, NV, P><<<static_cast<uint32_t>(grid), threads, 0, stream>>>(a, partial, parts);
+                typed(std::integral_constant<int, kDtF32>{});
             else
-                k_rms_norm_grad<kDtBf16, NV, P><<<static_cast<uint32_t>(grid), threads, 0, stream>>>(a, partial, parts);
+                typed(std::integral_constant<int, kDtBf16>{});
             note_launch("k_rms_norm_grad", kMapLinear, 1, grid, threads, NV);
         });
         const hipError_t e = hipGetLastError();

@@ -5,9 +5,9 @@
 // in the rows' type, in e4m3 with a scale for each block of 128 (the next
 // product's operand), or both.
 //
-// A wave takes 8 blocks of 128 columns of a row, a lane 16 columns, as the
-// quantiser of rows does.  Bound by HBM; rows past the last group are left
-// alone, and cost nothing but the end of a loop.
+// A wave takes 8 blocks of 128 columns of a row: twice 512 columns, a lane 8 of
+// each, so that its loads and stores take whole lines.  Bound by HBM; rows past
+// the last group are left alone, and cost nothing but the end of a loop.
 #include <algorithm>
 
 #include "block_common.h"
@@ -17,32 +17,38 @@ namespace {
 
 constexpr int kNone = -1;
 constexpr int kBlocksPerWave = 8;
-
-// The first `n` of sixteen values, rounded to the type.
-template <int DT>
-__device__ __forceinline__ void store16_values(char* p, int64_t n, const float (&v)[16]) {
-    store8<DT>(p, n, reinterpret_cast<const float(&)[8]>(v[0]));
-    store8<DT>(p + 8 * Arith<DT>::kEsize, n - 8, reinterpret_cast<const float(&)[8]>(v[8]));
-}
+constexpr int kSets = 2;                                  // of a wave's columns
+constexpr int kSetCols = kBlocksPerWave * kF8Block / kSets;  // 8 a lane
 
 struct Outputs {
     char* out;
     uint8_t* q;
     void* q_scale;
     int64_t cols, blocks, pitch;  // of a row of results
+    bool streamed;
 };
 
-// Sixteen results of columns c.. of a row, of which `n` exist.  All eight lanes of a block take part.
+// Eight results of columns c.. of a row, of which `n` exist; the others are zeros.  All 16 lanes of a block take part.
 template <int DT, int KIND>
-__device__ __forceinline__ void put(const Outputs& o, int64_t row, int64_t c, int64_t n, float (&v)[16]) {
-    if (o.out) store16_values<DT>(o.out + (row * o.cols + c) * Arith<DT>::kEsize, n, v);
+__device__ __forceinline__ void put(const Outputs& o, int64_t row, int64_t c, int64_t n, const float (&v)[8]) {
+    if (o.out) store8<DT>(o.out + (row * o.cols + c) * Arith<DT>::kEsize, n, v, o.streamed);
     if constexpr (KIND != kNone) {
+        uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = i < n ? v[i] : 0.0f;
-        const BlockScale s = block_scale<KIND>(max_oct(max_abs(v)));
+        for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
+        const BlockScale s = block_scale<KIND>(max16(m));
         const int64_t block = c / kF8Block;
-        if (block < o.blocks) *reinterpret_cast<uint4*>(o.q + row * o.blocks * kF8Block + c) = to_e4m3x16(v, s.r);
-        if ((threadIdx.x & 7) == 0 && block < o.pitch)
+        if (block < o.blocks) {
+            typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+            const u32x2_t q = {to_e4m3x4(v[0] * s.r, v[1] * s.r, v[2] * s.r, v[3] * s.r),
+                               to_e4m3x4(v[4] * s.r, v[5] * s.r, v[6] * s.r, v[7] * s.r)};
+            u32x2_t* const to = reinterpret_cast<u32x2_t*>(o.q + row * o.blocks * kF8Block + c);
+            if (o.streamed)
+                __builtin_nontemporal_store(q, to);
+            else
+                *to = q;
+        }
+        if ((threadIdx.x & 15) == 0 && block < o.pitch)
             store_scale<KIND>(o.q_scale, row * o.pitch + block, block < o.blocks ? s.kept : kScaleOne<KIND>);
     }
 }
@@ -52,24 +58,38 @@ __device__ __forceinline__ int64_t used_rows(const SwigluArgs& a) {
     return a.offsets ? group_offset(a.offsets, a.groups, a.rows) : a.rows;
 }
 
-template <int DT, int KIND>
-__global__ __launch_bounds__(kWG) void k_swiglu(SwigluArgs a, Outputs o, int chunks) {
-    constexpr int ES = Arith<DT>::kEsize;
-    const int lane = threadIdx.x & 63;
-    const int64_t items = used_rows(a) * chunks;
+// f(row, first column of this lane's first eight) for every set of columns of the rows in use.
+template <class F>
+__device__ __forceinline__ void for_items(int64_t rows, int chunks, F f) {
+    const int64_t items = rows * chunks;
     for (int64_t wg = blockIdx.x; wg * (kWG / 64) < items; wg += gridDim.x) {
         const int64_t item = wg * (kWG / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         if (item >= items) continue;
-        const int64_t row = item / chunks;
-        const int64_t c = ((item - row * chunks) * kBlocksPerWave + (lane >> 3)) * kF8Block + (lane & 7) * 16;
-        const char* const p = static_cast<const char*>(a.gu) + (row * 2 * a.inner + c) * ES;
-        float g[16], u[16];
-        load_values<DT>(p, a.inner - c, g);
-        load_values<DT>(p + a.inner * ES, a.inner - c, u);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) g[i] = g[i] * sigmoid(g[i]) * u[i];
-        put<DT, KIND>(o, row, c, a.inner - c, g);
+        // Up to 2^32 items the division takes a few instructions.
+        const int64_t row = items < (int64_t(1) << 32) ? static_cast<uint32_t>(item) / static_cast<uint32_t>(chunks) : item / chunks;
+        f(row, (item - row * chunks) * (kBlocksPerWave * kF8Block) + (threadIdx.x & 63) * 8);
     }
+}
+
+template <int DT, int KIND>
+__global__ __launch_bounds__(kWG) void k_swiglu(SwigluArgs a, Outputs o, int chunks) {
+    constexpr int ES = Arith<DT>::kEsize;
+    for_items(used_rows(a), chunks, [&](int64_t row, int64_t c) {
+        const char* const p = static_cast<const char*>(a.gu) + (row * 2 * a.inner + c) * ES;
+        float g[kSets][8], u[kSets][8];
+#pragma unroll
+        for (int s = 0; s < kSets; ++s) {
+            const int64_t n = a.inner - c - s * kSetCols;
+            load8<DT>(p + s * kSetCols * ES, n, g[s]);
+            load8<DT>(p + (a.inner + s * kSetCols) * ES, n, u[s]);
+        }
+#pragma unroll
+        for (int s = 0; s < kSets; ++s) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[s][i] = g[s][i] * sigmoid(g[s][i]) * u[s][i];
+            put<DT, KIND>(o, row, c + s * kSetCols, a.inner - c - s * kSetCols, g[s]);
+        }
+    });
 }
 
 __device__ __forceinline__ void gradients(float g, float u, float dh, float& dg, float& du) {
@@ -78,84 +98,80 @@ __device__ __forceinline__ void gradients(float g, float u, float dh, float& dg,
     du = dh * (g * s);
 }
 
-// A lane makes 16 columns of dg and the same of du.  Where results are quantised the halves have to be whole blocks.
+// A lane makes columns of dg and the same of du.  Where results are quantised the halves have to be whole blocks.
 template <int DT, int KIND>
 __global__ __launch_bounds__(kWG) void k_swiglu_grad(SwigluArgs a, Outputs o, int chunks) {
     constexpr int ES = Arith<DT>::kEsize;
-    const int lane = threadIdx.x & 63;
-    const int64_t items = used_rows(a) * chunks;
-    for (int64_t wg = blockIdx.x; wg * (kWG / 64) < items; wg += gridDim.x) {
-        const int64_t item = wg * (kWG / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (item >= items) continue;
-        const int64_t row = item / chunks;
-        const int64_t c = ((item - row * chunks) * kBlocksPerWave + (lane >> 3)) * kF8Block + (lane & 7) * 16;
-        const int64_t n = a.inner - c;
+    for_items(used_rows(a), chunks, [&](int64_t row, int64_t c) {
         const char* const p = static_cast<const char*>(a.gu) + (row * 2 * a.inner + c) * ES;
-        float g[16], u[16], dh[16];
-        load_values<DT>(p, n, g);
-        load_values<DT>(p + a.inner * ES, n, u);
-        load_values<DT>(static_cast<const char*>(a.dout) + (row * a.inner + c) * ES, n, dh);
+        const char* const d = static_cast<const char*>(a.dout) + (row * a.inner + c) * ES;
+        float g[kSets][8], u[kSets][8], dh[kSets][8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) gradients(g[i], u[i], dh[i], g[i], u[i]);
-        if (n <= 0) continue;
-        put<DT, KIND>(o, row, c, n, g);
-        put<DT, KIND>(o, row, a.inner + c, n, u);
-        if constexpr (KIND != kNone) {
-            // The entries of the scales past the last block, which no lane's columns reach.
-            if (c == 0 && o.blocks < o.pitch)
-                for (int64_t b = o.blocks; b < o.pitch; ++b) store_scale<KIND>(o.q_scale, row * o.pitch + b, kScaleOne<KIND>);
+        for (int s = 0; s < kSets; ++s) {
+            const int64_t n = a.inner - c - s * kSetCols;
+            load8<DT>(p + s * kSetCols * ES, n, g[s]);
+            load8<DT>(p + (a.inner + s * kSetCols) * ES, n, u[s]);
+            load8<DT>(d + s * kSetCols * ES, n, dh[s]);
         }
-    }
+#pragma unroll
+        for (int s = 0; s < kSets; ++s) {
+            const int64_t at = c + s * kSetCols, n = a.inner - at;
+            if (n <= 0) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) gradients(g[s][i], u[s][i], dh[s][i], g[s][i], u[s][i]);
+            put<DT, KIND>(o, row, at, n, g[s]);
+            put<DT, KIND>(o, row, a.inner + at, n, u[s]);
+            if constexpr (KIND != kNone) {
+                // The entries of the scales past the last block, which no lane's columns reach.
+                if (at == 0)
+                    for (int64_t b = o.blocks; b < o.pitch; ++b) store_scale<KIND>(o.q_scale, row * o.pitch + b, kScaleOne<KIND>);
+            }
+        }
+    });
 }
 
-// Halves that are no whole blocks, quantised: a lane makes 16 columns of the row of results, whichever half they are of,
+// Halves that are no whole blocks, quantised: a lane makes 8 columns of the row of results, whichever half they are of,
 // and reads what it needs of both; a block that holds columns of both halves has one scale.
 template <int DT, int KIND>
 __global__ __launch_bounds__(kWG) void k_swiglu_grad_across(SwigluArgs a, Outputs o, int chunks) {
     constexpr int ES = Arith<DT>::kEsize;
-    const int lane = threadIdx.x & 63;
-    const int64_t items = used_rows(a) * chunks;
-    for (int64_t wg = blockIdx.x; wg * (kWG / 64) < items; wg += gridDim.x) {
-        const int64_t item = wg * (kWG / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (item >= items) continue;
-        const int64_t row = item / chunks;
-        const int64_t c = ((item - row * chunks) * kBlocksPerWave + (lane >> 3)) * kF8Block + (lane & 7) * 16;
+    using Raw = typename Arith<DT>::Raw;
+    for_items(used_rows(a), chunks, [&](int64_t row, int64_t c0) {
         const char* const gu = static_cast<const char*>(a.gu) + row * 2 * a.inner * ES;
         const char* const dout = static_cast<const char*>(a.dout) + row * a.inner * ES;
-        float v[16] = {};
-        // One half, from column `from` of it on, into v from `at` on.
-        const auto half = [&](int64_t from, int64_t n, bool up_half) {
-            float g[16], u[16], dh[16];
-            load_values<DT>(gu + from * ES, n, g);
-            load_values<DT>(gu + (a.inner + from) * ES, n, u);
-            load_values<DT>(dout + from * ES, n, dh);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float dg, du;
-                gradients(g[i], u[i], dh[i], dg, du);
-                v[i] = up_half ? du : dg;
-            }
-        };
-        if (c + 16 <= a.inner) {
-            half(c, 16, false);
-        } else if (c >= a.inner) {
-            half(c - a.inner, 2 * a.inner - c, true);
-        } else {
+        for (int s = 0; s < kSets; ++s) {
+            const int64_t c = c0 + s * kSetCols;
+            float v[8] = {};
+            if (c + 8 <= a.inner || c >= a.inner) {
+                const bool up_half = c >= a.inner;
+                const int64_t from = up_half ? c - a.inner : c, n = a.inner - from;
+                float g[8], u[8], dh[8];
+                load8<DT>(gu + from * ES, n, g);
+                load8<DT>(gu + (a.inner + from) * ES, n, u);
+                load8<DT>(dout + from * ES, n, dh);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const bool up_half = c + i >= a.inner;
-                const int64_t j = up_half ? c + i - a.inner : c + i;
-                if (j >= a.inner) continue;
-                using Raw = typename Arith<DT>::Raw;
-                float dg, du;
-                gradients(Arith<DT>::widen1(reinterpret_cast<const Raw*>(gu)[j]),
-                          Arith<DT>::widen1(reinterpret_cast<const Raw*>(gu)[a.inner + j]),
-                          Arith<DT>::widen1(reinterpret_cast<const Raw*>(dout)[j]), dg, du);
-                v[i] = up_half ? du : dg;
+                for (int i = 0; i < 8; ++i) {
+                    float dg, du;
+                    gradients(g[i], u[i], dh[i], dg, du);
+                    v[i] = up_half ? du : dg;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool up_half = c + i >= a.inner;
+                    const int64_t j = up_half ? c + i - a.inner : c + i;
+                    if (j >= a.inner) continue;
+                    float dg, du;
+                    gradients(Arith<DT>::widen1(reinterpret_cast<const Raw*>(gu)[j]),
+                              Arith<DT>::widen1(reinterpret_cast<const Raw*>(gu)[a.inner + j]),
+                              Arith<DT>::widen1(reinterpret_cast<const Raw*>(dout)[j]), dg, du);
+                    v[i] = up_half ? du : dg;
+                }
             }
+            put<DT, KIND>(o, row, c, 2 * a.inner - c, v);
         }
-        put<DT, KIND>(o, row, c, 2 * a.inner - c, v);
-    }
+    });
 }
 
 template <class F>
@@ -175,7 +191,7 @@ void by_types(const SwigluArgs& a, F f) {
 }
 
 Outputs outputs(const SwigluArgs& a, int64_t cols) {
-    return {static_cast<char*>(a.out), static_cast<uint8_t*>(a.q), a.q_scale, cols, f8_width(cols) / kF8Block, f8_pitch(cols)};
+    return {static_cast<char*>(a.out), static_cast<uint8_t*>(a.q), a.q_scale, cols, f8_width(cols) / kF8Block, f8_pitch(cols), a.streamed};
 }
 
 // Waves of a row whose blocks, with the entries past the last scale, number `blocks`; and workgroups for all rows.

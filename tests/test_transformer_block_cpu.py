@@ -22,7 +22,7 @@ def test_norm_refuses():
         (dict(x=None), INVALID), (dict(w=None), INVALID), (dict(sum=None), INVALID), (dict(q=None), INVALID), (dict(qs=None), INVALID),
         (dict(out=None, q=None, qs=None), INVALID), (dict(res=None), INVALID), (dict(dtype=2), UNSUPPORTED), (dict(dtype=nuna.F32), UNSUPPORTED),
         (dict(wd=5), UNSUPPORTED), (dict(kind=2), UNSUPPORTED), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID),
-        (dict(eps=float("inf")), INVALID), (dict(cols=0), INVALID), (dict(cols=32769, xs=40000, rs=40000, ss=40000), UNSUPPORTED),
+        (dict(eps=float("inf")), INVALID), (dict(cols=0), INVALID), (dict(cols=16385, xs=40000, rs=40000, ss=40000), UNSUPPORTED),
         (dict(rows=1 << 31), INVALID), (dict(xs=511), INVALID), (dict(rs=-1), INVALID), (dict(ss=100), INVALID), (dict(x=P[0] + 8), MISALIGNED),
         (dict(w=P[2] + 2), MISALIGNED), (dict(rstd=P[7] + 2), MISALIGNED), (dict(out=P[4] + 8), MISALIGNED), (dict(q=P[5] + 8), MISALIGNED),
         (dict(out=P[0]), OVERLAP), (dict(sum=P[0] + 1024), OVERLAP), (dict(sum=P[1], ss=520), OVERLAP), (dict(sum=P[0], ss=520), OVERLAP),

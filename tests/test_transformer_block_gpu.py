@@ -2,7 +2,7 @@
 SwiGLU, their gradients, and the expert layer of a few tokens, at the sizes, masks and strides where they can go wrong.
 
 Bounds.  Whole numbers are compared for equality.  A rounding to bf16 costs 2^-8 of the value, to fp32 2^-24 = EPS.  A sum
-of a row's n values is formed by threads of at most 32 values, then over 16 lanes, 4 rows of lanes and 16 waves: fewer than
+of a row's n values is formed by threads of at most 16 values, then over 16 lanes, 4 rows of lanes and 16 waves: fewer than
 64 roundings, each of at most EPS of the sum of the magnitudes.  The bounds of each operator stand at its tests.
 
 These tests make streams of their own; the tests that pin the map of workgroups to XCDs come before this file."""
@@ -61,7 +61,7 @@ def check_quantized(q, scale, want, slack, kind, used=None):
 # products: 40 EPS of y in all, before its rounding.
 
 NORM_SLACK = 40 * EPS
-WIDTHS = [1, 7, 8, 100, 128, 129, 200, 256, 400, 512, 520, 1000, 1024, 1032, 2880, 4097, 7168, 8192, 8200, 16384, 20001, 32768]
+WIDTHS = [1, 7, 8, 100, 128, 129, 200, 256, 400, 512, 520, 1000, 1024, 1032, 2880, 4097, 7168, 8192, 8200, 12001, 16384]
 
 
 @pytest.mark.parametrize("H", WIDTHS)
@@ -82,7 +82,7 @@ def test_norm(nuna, T, H, dtype):
     assert torch.equal(again, out)
 
 
-@pytest.mark.parametrize("H", [1, 100, 128, 384, 640, 1000, 2888, 7168, 9000, 17000])
+@pytest.mark.parametrize("H", [1, 100, 128, 384, 640, 1000, 2888, 7168, 9000, 16000])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("kind", ["f32", "e8m0"])
 @pytest.mark.parametrize("both", [False, True])
@@ -142,7 +142,7 @@ def test_norm_of_many_rows_and_of_none(nuna):
 
 # dx: zr is one product off, u one; the sum of u zr 66 EPS of its magnitudes; then five roundings of dx's parts.
 @pytest.mark.parametrize("T,H", [(1, 1), (3, 128), (40, 100), (70, 200), (33, 300), (21, 512), (9, 1000), (5, 1032), (600, 136),
-                                 (17, 2880), (530, 1100), (7, 7168), (3, 8200), (2, 32767)])
+                                 (17, 2880), (530, 1100), (7, 7168), (3, 8200), (2, 16383), (530, 8192)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("residual", [False, True])
 def test_norm_grad(nuna, T, H, dtype, residual):
