@@ -121,14 +121,14 @@ __device__ __forceinline__ float sum_lanes(float v) {
 }
 
 // 1 / (1 + exp(-g)), about as exact as with the library's exponential and a division, at a third of their instructions; 0
-// below -87 (where it is under 2^-125).  The exponent is kept in two parts, so that its rounding does not grow with g, and
-// the reciprocal is improved once.
+// below -87 (where it is under 2^-125).  exp(x) = 2^h exp(x - h ln 2) with h = x log2(e) as it is rounded, whose error
+// would grow with x, and the second factor by its first two terms.  (ln 2 is 1.9e-9 off: a third of a last place for
+// each 10 of x.)  The reciprocal is improved once.
 __device__ __forceinline__ float sigmoid(float g) {
     const float x = -__builtin_amdgcn_fmed3f(g, -87.0f, 87.0f);
-    const float hi = x * 1.44269502f;  // log2(e) = 1.44269502 + 1.9259630e-8
-    const float lo = fmaf(x, 1.9259630e-8f, fmaf(x, 1.44269502f, -hi));
-    float e = __builtin_amdgcn_exp2f(hi);
-    e = fmaf(e, lo * 0.693147182f, e);
+    const float h = x * 1.44269502f;
+    float e = __builtin_amdgcn_exp2f(h);
+    e = fmaf(e, fmaf(-h, 0.693147182f, x), e);
     const float d = 1.0f + e;
     float s = __builtin_amdgcn_rcpf(d);
     s = fmaf(fmaf(-d, s, 1.0f), s, s);

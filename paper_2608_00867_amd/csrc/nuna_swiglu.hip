@@ -71,23 +71,26 @@ __device__ __forceinline__ void for_items(int64_t rows, int chunks, F f) {
     }
 }
 
-template <int DT, int KIND>
+template <int DT, int KIND, bool WHOLE>
 __global__ __launch_bounds__(kWG) void k_swiglu(SwigluArgs a, Outputs o, int chunks) {
     constexpr int ES = Arith<DT>::kEsize;
     for_items(used_rows(a), chunks, [&](int64_t row, int64_t c) {
-        const char* const p = static_cast<const char*>(a.gu) + (row * 2 * a.inner + c) * ES;
-        float g[kSets][8], u[kSets][8];
+        const char* const p = static_cast<const char*>(a.gu) + row * 2 * a.inner * ES;
+        Raw8<DT> rg[kSets], ru[kSets];
 #pragma unroll
         for (int s = 0; s < kSets; ++s) {
-            const int64_t n = a.inner - c - s * kSetCols;
-            load8<DT>(p + s * kSetCols * ES, n, g[s]);
-            load8<DT>(p + (a.inner + s * kSetCols) * ES, n, u[s]);
+            rg[s] = load_raw8<DT, WHOLE>(p, c + s * kSetCols, a.inner);
+            ru[s] = load_raw8<DT, WHOLE>(p + a.inner * ES, c + s * kSetCols, a.inner);
         }
 #pragma unroll
         for (int s = 0; s < kSets; ++s) {
+            const int64_t n = a.inner - c - s * kSetCols;
+            float g[8], u[8];
+            widen<DT>(rg[s], n > 0, g);
+            widen<DT>(ru[s], n > 0, u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) g[s][i] = g[s][i] * sigmoid(g[s][i]) * u[s][i];
-            put<DT, KIND>(o, row, c + s * kSetCols, a.inner - c - s * kSetCols, g[s]);
+            for (int i = 0; i < 8; ++i) g[i] = g[i] * sigmoid(g[i]) * u[i];
+            put<DT, KIND>(o, row, c + s * kSetCols, n, g);
         }
     });
 }
@@ -99,28 +102,31 @@ __device__ __forceinline__ void gradients(float g, float u, float dh, float& dg,
 }
 
 // A lane makes columns of dg and the same of du.  Where results are quantised the halves have to be whole blocks.
-template <int DT, int KIND>
+template <int DT, int KIND, bool WHOLE>
 __global__ __launch_bounds__(kWG) void k_swiglu_grad(SwigluArgs a, Outputs o, int chunks) {
     constexpr int ES = Arith<DT>::kEsize;
     for_items(used_rows(a), chunks, [&](int64_t row, int64_t c) {
-        const char* const p = static_cast<const char*>(a.gu) + (row * 2 * a.inner + c) * ES;
-        const char* const d = static_cast<const char*>(a.dout) + (row * a.inner + c) * ES;
-        float g[kSets][8], u[kSets][8], dh[kSets][8];
+        const char* const p = static_cast<const char*>(a.gu) + row * 2 * a.inner * ES;
+        const char* const d = static_cast<const char*>(a.dout) + row * a.inner * ES;
+        Raw8<DT> rg[kSets], ru[kSets], rd[kSets];
 #pragma unroll
         for (int s = 0; s < kSets; ++s) {
-            const int64_t n = a.inner - c - s * kSetCols;
-            load8<DT>(p + s * kSetCols * ES, n, g[s]);
-            load8<DT>(p + (a.inner + s * kSetCols) * ES, n, u[s]);
-            load8<DT>(d + s * kSetCols * ES, n, dh[s]);
+            rg[s] = load_raw8<DT, WHOLE>(p, c + s * kSetCols, a.inner);
+            ru[s] = load_raw8<DT, WHOLE>(p + a.inner * ES, c + s * kSetCols, a.inner);
+            rd[s] = load_raw8<DT, WHOLE>(d, c + s * kSetCols, a.inner);
         }
 #pragma unroll
         for (int s = 0; s < kSets; ++s) {
             const int64_t at = c + s * kSetCols, n = a.inner - at;
             if (n <= 0) continue;
+            float g[8], u[8], dh[8];
+            widen<DT>(rg[s], true, g);
+            widen<DT>(ru[s], true, u);
+            widen<DT>(rd[s], true, dh);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) gradients(g[s][i], u[s][i], dh[s][i], g[s][i], u[s][i]);
-            put<DT, KIND>(o, row, at, n, g[s]);
-            put<DT, KIND>(o, row, a.inner + at, n, u[s]);
+            for (int i = 0; i < 8; ++i) gradients(g[i], u[i], dh[i], g[i], u[i]);
+            put<DT, KIND>(o, row, at, n, g);
+            put<DT, KIND>(o, row, a.inner + at, n, u);
             if constexpr (KIND != kNone) {
                 // The entries of the scales past the last block, which no lane's columns reach.
                 if (at == 0)
@@ -207,7 +213,11 @@ hipError_t launch_swiglu(const SwigluArgs& a, hipStream_t stream) {
     const int chunks = chunks_of(a.q ? o.pitch : o.blocks);
     const int64_t grid = grid_of(a.rows, chunks);
     by_types(a, [&](auto dt, auto kind) {
-        k_swiglu<decltype(dt)::value, decltype(kind)::value><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(a, o, chunks);
+        constexpr int DT = decltype(dt)::value, KIND = decltype(kind)::value;
+        if (a.inner % 8 == 0)
+            k_swiglu<DT, KIND, true><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(a, o, chunks);
+        else
+            k_swiglu<DT, KIND, false><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(a, o, chunks);
     });
     note_launch("k_swiglu", kMapLinear, 1, grid, kWG, 1);
     return hipGetLastError();
@@ -225,7 +235,10 @@ hipError_t launch_swiglu_grad(const SwigluArgs& a, hipStream_t stream) {
                 k_swiglu_grad_across<DT, KIND><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(a, o, chunks);
                 return;
             }
-        k_swiglu_grad<DT, KIND><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(a, o, chunks);
+        if (a.inner % 8 == 0)
+            k_swiglu_grad<DT, KIND, true><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(a, o, chunks);
+        else
+            k_swiglu_grad<DT, KIND, false><<<static_cast<uint32_t>(grid), kWG, 0, stream>>>(a, o, chunks);
     });
     note_launch(across ? "k_swiglu_grad_across" : "k_swiglu_grad", kMapLinear, 1, grid, kWG, 1);
     return hipGetLastError();
