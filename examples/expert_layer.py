@@ -2,11 +2,12 @@
 
     python examples/expert_layer.py [--ranks 8] [--tokens 128] [--hidden 2048] [--inner 1024] [--experts 64] [--topk 4]
 
-Every rank's tokens are dispatched to the ranks of their experts (all_to_all), each rank sorts the slots of the rows that
-it received by expert, gathers and quantises the rows, multiplies them by its experts' 8-bit weights (two products with
-SwiGLU between them), and scatters the results back, weighted by the router; the ranks' sums are combined
-(all_to_all_combine).  The backward pass of one rank's part follows: the gradients of the rows, of the router's weights
-and of both weight matrices.  The results are compared with a plain fp32 layer on the unquantised weights.
+The router chooses every token's experts and their weights, and every rank's tokens are dispatched to the ranks of their
+experts (all_to_all).  Each rank sorts the slots of the rows that it received by expert, gathers and quantises the rows,
+multiplies them by its experts' 8-bit weights (two products with SwiGLU between them), and scatters the results back,
+weighted by the router; the ranks' sums are combined (all_to_all_combine).  The backward pass of one rank's part follows:
+the gradients of the rows, of the router's weights and of both weight matrices.  The results are compared with a plain fp32
+layer on the unquantised weights.
 """
 import argparse
 import os
@@ -39,28 +40,23 @@ class Experts:
         xq = torch.empty((room, nuna.f8_width(hidden)), dtype=torch.float8_e4m3fn, device=x.device)
         xs = torch.empty((room, nuna.f8_pitch(hidden)), dtype=torch.float8_e8m0fnu, device=x.device)
         nuna.moe_gather(x, row_of, xq, xs)
-        # Rows past the last are not written by the products: zeros, as the activation runs over all of them.
-        gu = torch.zeros((room, self.w1[0].shape[1]), dtype=x.dtype, device=x.device)
+        gu = torch.empty((room, self.w1[0].shape[1]), dtype=x.dtype, device=x.device)
         nuna.f8_matmul(xq, xs, *self.w1, gu, offsets=offsets)
-        gate, up = gu.float().chunk(2, 1)
-        h = (torch.nn.functional.silu(gate) * up).to(x.dtype)
+        h = torch.empty((room, gu.shape[1] // 2), dtype=x.dtype, device=x.device)
         y = torch.zeros((room, hidden), dtype=x.dtype, device=x.device)
-        nuna.f8_matmul(*nuna.f8_quantize(h, SCALE), *self.w2, y, offsets=offsets)
+        nuna.f8_matmul(*nuna.swiglu(gu, offsets, SCALE, out=h), *self.w2, y, offsets=offsets)
         return nuna.moe_scatter(y, row_of, weights), (x, offsets, slot_of, row_of, topk.shape[1], weights, gu, h, y)
 
     def backward(self, dout, saved):
         """(dx, dweights, dw1, dw2); the weights' gradients in fp32."""
         x, offsets, slot_of, row_of, k, weights, gu, h, y = saved
         dy, dweights = nuna.moe_scatter_grad(dout, y, row_of, weights)
-        dh = torch.zeros_like(h)
+        dh = torch.empty_like(h)
         nuna.f8_matmul(*nuna.f8_quantize(dy, SCALE), *self.w2_t, dh, offsets=offsets)
         dw2 = nuna.f8_wgrad(*nuna.f8_quantize_cols(dy, offsets, SCALE), *nuna.f8_quantize_cols(h, offsets, SCALE), offsets)
-        gate, up = gu.float().chunk(2, 1)
-        s = torch.sigmoid(gate)
-        dgate = dh.float() * up * (s + gate * s * (1 - s))
-        dgu = torch.cat([dgate, dh.float() * gate * s], 1).to(x.dtype)
+        dgu = torch.empty_like(gu)
         dx_rows = torch.zeros((dgu.shape[0], x.shape[1]), dtype=x.dtype, device=x.device)
-        nuna.f8_matmul(*nuna.f8_quantize(dgu, SCALE), *self.w1_t, dx_rows, offsets=offsets)
+        nuna.f8_matmul(*nuna.swiglu_grad(dh, gu, offsets, SCALE, out=dgu), *self.w1_t, dx_rows, offsets=offsets)
         dw1 = nuna.f8_wgrad(*nuna.f8_quantize_cols(dgu, offsets, SCALE),
                             *nuna.f8_quantize_cols(x, offsets, SCALE, slot_of=slot_of, topk=k), offsets)
         return nuna.moe_scatter(dx_rows, row_of), dweights, dw1, dw2
@@ -88,8 +84,8 @@ def run(ranks=8, tokens=128, hidden=2048, inner=1024, experts=64, topk=4, seed=0
     randn = lambda *s: torch.randn(s, generator=gen, device=dev)  # noqa: E731
     count = experts // ranks
     x = [randn(tokens, hidden).bfloat16() for _ in range(ranks)]
-    weights, table = torch.softmax(randn(ranks, tokens, experts), 2).topk(topk, 2)
-    weights, table = weights.contiguous(), table.to(torch.int32).contiguous()
+    table, weights = nuna.route_topk(randn(ranks * tokens, experts), topk, normalize=False)
+    table, weights = table.view(ranks, tokens, topk), weights.view(ranks, tokens, topk)
     w1 = (randn(experts, 2 * inner, hidden) / hidden ** 0.5).bfloat16()
     w2 = (randn(experts, hidden, inner) / inner ** 0.5).bfloat16()
     parts = [Experts(w1[r * count:(r + 1) * count], w2[r * count:(r + 1) * count], r * count) for r in range(ranks)]

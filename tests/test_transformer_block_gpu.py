@@ -286,6 +286,23 @@ def test_route_rows_that_are_masked_or_not_finite(nuna):
             assert (d[0] == 0).all()
 
 
+@pytest.mark.parametrize("E,k", [(6, 6), (100, 64), (256, 8), (256, 64), (1024, 64)])
+@pytest.mark.parametrize("T", [9, 1500])
+def test_route_chooses_in_bf16_as_in_fp32(nuna, T, E, k):
+    """The same numbers in both types, many of them equal, few of them or none in some rows, some not finite."""
+    g = np.random.default_rng(E + k)
+    z = np.round(g.standard_normal((T, E)) * 2) / 2
+    z[g.random((T, E)) < g.random((T, 1))] = -np.inf
+    z[0], z[1], z[2, 1:] = -np.inf, 0.0, -np.inf
+    z[3, 2::3], z[4, 1::2], z[5], z[6, E // 2:] = np.nan, np.inf, -0.0, -3e38
+    t = torch.from_numpy(z).to(torch.bfloat16).cuda()
+    narrow, wide = nuna.route_topk(t, k), nuna.route_topk(t.float(), k)
+    assert torch.equal(narrow[0], wide[0])
+    assert torch.equal(narrow[1].view(torch.int32)[7:], wide[1].view(torch.int32)[7:])
+    rows = [0, 1, 2, 4, 5, 6, 7, 8]
+    assert np.array_equal(host(narrow[0])[rows], blk.choose(t[rows].double().cpu().numpy(), k))
+
+
 def test_route_biased_choice_near_a_border(nuna):
     """Scores that fp32's sigmoids cannot tell apart."""
     z = torch.full((64, 40), 3.0)
