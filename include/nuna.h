@@ -687,8 +687,8 @@ nuna_status_t nuna_swiglu_grad(const void* dout, const void* gu, const int32_t* 
  * A whole expert layer for a few tokens (a decode step), in two kernels:
  *   out[t] = sum over j of weights[t][j] * W2[e] SwiGLU(W1[e] x[t]),  e = topk_idx[t][j]
  * over the entries with an expert in [first_expert, first_expert + num_experts);
- * a token with none gets zeros.  Every reached expert's weights are read once
- * for up to 16 tokens; nothing is sorted or gathered.
+ * a token with none gets zeros.  Every reached expert's weights are read once;
+ * nothing is sorted or gathered.
  *   x         [tokens][x_stride >= hidden] of dtype
  *   topk_idx  int32 [tokens][topk], any numbers;  weights fp32 [tokens][topk]
  *   w1        8-bit [num_experts][2 * inner][kp of hidden], w1_scale

@@ -17,6 +17,11 @@
 //
 // As in the 8-bit products the weights are the first operand, so that lane l
 // holds the outputs x = 4 (l / 16) + i of row y = l % 16.
+//
+// Rates, of the weights' bytes alone.  One token, 8 experts of 7168 x 2048 (352
+// MB): 48.4 us for the first products, 4.9 TB/s, and 24.8 for the second, 4.7;
+// reads of the same lines with nothing else take 38.8 and 20.  64 tokens on 30
+// of 32 such experts: 160 and 71 us, 5.9 and 6.2 TB/s.
 #include <algorithm>
 
 #include "block_common.h"
@@ -65,7 +70,8 @@ struct Routing {
     int count;
 };
 
-// Fills it in.  Up to 64 slots every wave finds the experts by itself, in the order of their first slots.
+// Fills it in.  Up to 64 slots the first wave finds the experts in registers, in the order of their first slots; of more they
+// are marked in a bitmap, in ascending order.
 __device__ __forceinline__ void find_experts(const FewArgs& a, Routing& r) {
     const int slots = a.tokens * a.topk;
     const bool few = slots <= 64;

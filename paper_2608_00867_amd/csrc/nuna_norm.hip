@@ -10,7 +10,14 @@
 //
 // A row stays in registers between its sum of squares and its outputs, eight
 // values a thread and chunk, so every value is read once and 16 lanes hold a
-// block of 128 with its scale.  Both are bound by HBM, few rows by latency.
+// block of 128 with its scale.  Rows wider than 1024 have a workgroup of their
+// own: a row's sum then costs one barrier, and the next row's loads, made
+// before it, cover the wait (rows of 2880, bf16: 35 us, without them 41).
+//
+// Both are bound by HBM.  8195 rows of 2880 with a residual: 34.2 us, 5.5 TB/s
+// of the 189 MB that have to move; the gradient of 4096 rows of 7168, 235 MB:
+// 47.3 us, 5.0 TB/s, and 5.4 for the sum of the 512 parts of dw.  Few rows are
+// bound by latency: 64 of 7168 take 4.9 us.
 #include <algorithm>
 
 #include "block_common.h"

@@ -11,13 +11,18 @@
 //   sigmoid, normalised  dz_j = f q_j (1 - p_j) (g_j - <q, g>)
 //   sigmoid              dz_j = f g_j p_j (1 - p_j)
 //
-// L lanes hold a token's logits, N consecutive ones each, as integers that
+// L lanes (16, where that still fills the card, or 64) hold a token's logits, N consecutive ones each, as integers that
 // order as the numbers do (0: cannot be chosen, or taken).  A choice is the
 // largest of the lanes' largest, of the first lane that has it; only that
 // lane looks for its next largest.  The biased choice compares scores that lie
 // closer together than fp32's sigmoids are exact, so it is made in fp64.
 // Normalised weights do not depend on what all scores have in common, and are
 // formed relative to the largest, so that they cannot vanish together.
+//
+// Bound by instructions: a choice looks at each of a lane's keys once.  32771
+// tokens, 8 of 256 in bf16: 11.6 us, of which the 17 MB of logits are 2.6 and a
+// launch 2.8; the gradient of 16384 tokens with 32 experts 6.2 us.  64 tokens
+// take 6.8 us, the wait for the logits and the fp64 sigmoids of a biased choice.
 #include <algorithm>
 
 #include "block_common.h"

@@ -6,8 +6,15 @@
 // product's operand), or both.
 //
 // A wave takes 8 blocks of 128 columns of a row: twice 512 columns, a lane 8 of
-// each, so that its loads and stores take whole lines.  Bound by HBM; rows past
-// the last group are left alone, and cost nothing but the end of a loop.
+// each, so that its loads and stores take whole lines.  All of a wave's loads
+// are made before the first is used, at addresses cut to the row, outside of
+// any branch: a load in a branch is waited for at its end (16384 rows of 2048
+// to e4m3: 35.8 us, with such branches 41.6).  Rows past the last group are
+// left alone, and cost nothing but the end of a loop.
+//
+// Bound by HBM: those 16384 rows move 168 MB, 4.7 TB/s; 16396 rows of 2888 to
+// both types 63 us, 5.2 TB/s; the gradient of 4096 rows of 2048 to both types
+// 22.3 us, 4.5 TB/s.
 #include <algorithm>
 
 #include "block_common.h"
