@@ -694,3 +694,88 @@ def test_wrong_calls_raise(nuna):
     big, many = x.repeat(17, 1), idx.repeat(17, 1)
     with pytest.raises(nuna.NunaError):
         nuna.expert_layer_few(big, many, wt.repeat(17, 1), *packed)
+
+
+# ------------------------------------------------------------------ offsets past 32 bits, the widest layer
+
+def same_rows(got, want):
+    return torch.equal(got.contiguous().view(torch.uint8), want.contiguous().view(torch.uint8))
+
+
+def far_rows(rows, cols, seed):
+    """bf16 [rows, cols] whose last 64 rows hold numbers; more than 2^32 bytes."""
+    t = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    assert t.numel() * 2 > 2 ** 32
+    t[-64:] = values((64, cols), "bf16", seed)[0]
+    return t
+
+
+def test_norm_and_its_gradient_far_out(nuna):
+    T, H = 270000, 8192
+    x, w = far_rows(T, H, 1), values((H,), "bf16", 2)[0]
+    rstd = torch.empty(T, device="cuda")
+    out = torch.empty_like(x)
+    q, s = nuna.rms_norm(x, w, scale="f32", out=out, rstd=rstd)
+    near_r = torch.empty(64, device="cuda")
+    near = torch.empty((64, H), dtype=x.dtype, device="cuda")
+    nq, ns = nuna.rms_norm(x[-64:], w, scale="f32", out=near, rstd=near_r)
+    assert all(same_rows(a[-64:], b) for a, b in ((q, nq), (s, ns), (out, near), (rstd, near_r)))
+    assert bool((out[:-64] == 0).all())
+    dx, dw = nuna.rms_norm_grad(out, x, w, rstd)
+    near_dx, near_dw = nuna.rms_norm_grad(near, x[-64:], w, near_r)
+    assert same_rows(dx[-64:], near_dx)
+    # The same 64 terms, and zeros, in another order: 64 roundings of the terms' magnitudes.
+    terms = (near.double() * x[-64:].double() * near_r.double().unsqueeze(1)).abs().sum(0)
+    assert bool(((dw - near_dw).double().abs() <= 2 * 66 * EPS * terms).all())
+
+
+def test_swiglu_and_its_gradient_far_out(nuna):
+    rows, inner = 270000, 4096
+    gu = far_rows(rows, 2 * inner, 3)
+    dh = torch.zeros((rows, inner), dtype=gu.dtype, device="cuda")
+    dh[-64:] = values((64, inner), "bf16", 4)[0]
+    offsets = torch.tensor([0, 5, rows], dtype=torch.int32, device="cuda")
+    q, s = nuna.swiglu(gu, offsets, "e8m0")
+    nq, ns = nuna.swiglu(gu[-64:], scale="e8m0")
+    assert same_rows(q[-64:], nq) and same_rows(s[-64:], ns)
+    assert same_rows(nuna.swiglu_grad(dh, gu, offsets)[-64:], nuna.swiglu_grad(dh[-64:], gu[-64:]))
+
+
+def test_router_far_out(nuna):
+    T, E, k = 2 ** 21 + 3, 1024, 2
+    z = far_rows(T, E, 5)
+    idx, w = nuna.route_topk(z, k)
+    near_i, near_w = nuna.route_topk(z[-64:], k)
+    assert torch.equal(idx[-64:], near_i) and same_rows(w[-64:], near_w)
+    assert bool((idx[:-64] == torch.arange(k, device="cuda")).all())
+    assert same_rows(nuna.route_topk_grad(w, z, idx)[-64:], nuna.route_topk_grad(near_w, z[-64:], near_i))
+
+
+def test_few_widest_layer(nuna):
+    """65536 x 65536: matrices of 2^33 and 2^32 bytes.  A sum is of 64 blocks a wave, 8 waves and fewer than 24 roundings in a
+    block, so off by at most 96 EPS of its terms' magnitudes, which are about sqrt(65536) times the sum (2-norm): 256 * 96 EPS =
+    1.5e-3 a product, and twice that behind the activation."""
+    n = 65536
+    gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def matrix(rows):
+        w = torch.empty((1, rows, n), dtype=torch.uint8, device="cuda")
+        for r in range(0, rows, 4096):
+            w[0, r:r + 4096] = torch.randint(0, 0x7f, (4096, n), dtype=torch.uint8, device="cuda", generator=gen)
+            w[0, r:r + 4096] |= torch.randint(0, 2, (4096, n), dtype=torch.uint8, device="cuda", generator=gen) << 7
+        s = torch.rand((1, rows // 128, n // 128), device="cuda", generator=gen) / (n ** 0.5 * 64)
+        return w.view(torch.float8_e4m3fn), s
+
+    def product(w, s, v):
+        out = torch.empty(w.shape[1], dtype=torch.float64, device="cuda")
+        for r in range(0, w.shape[1], 4096):
+            each = w[0, r:r + 4096].float().view(32, 128, n // 128, 128).double() * s[0, r // 128:r // 128 + 32].double()[:, None, :, None]
+            out[r:r + 4096] = (each.view(4096, n) * v).sum(1)
+        return out
+    w1, w2 = matrix(2 * n), matrix(n)
+    x = torch.randn((1, n), device="cuda", generator=gen)
+    out = nuna.expert_layer_few(x, torch.tensor([[3]], dtype=torch.int32, device="cuda"), torch.tensor([[0.5]], device="cuda"),
+                                *w1, *w2, first_expert=3)
+    gate, up = product(*w1, x[0].double()).chunk(2)
+    want = product(*w2, 0.5 * gate * torch.sigmoid(gate) * up)
+    assert ((out[0].double() - want).norm() / want.norm()).item() <= 5e-3
