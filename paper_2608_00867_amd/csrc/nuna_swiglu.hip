@@ -5,16 +5,18 @@
 // in the rows' type, in e4m3 with a scale for each block of 128 (the next
 // product's operand), or both.
 //
-// A wave takes 8 blocks of 128 columns of a row: twice 512 columns, a lane 8 of
-// each, so that its loads and stores take whole lines.  All of a wave's loads
-// are made before the first is used, at addresses cut to the row, outside of
+// A wave takes 4 blocks of 128 columns of a row, a lane 8 columns, so that its
+// loads and stores take whole lines, and no more than that: other waves do
+// better than a wave's own next loads (16396 rows of 2888 to both types: 60 us;
+// 8 blocks a wave 63; waves that stay and load the next item while one is
+// stored 66 to 72).  All of a wave's loads are made before the first is used, at addresses cut to the row, outside of
 // any branch: a load in a branch is waited for at its end (16384 rows of 2048
-// to e4m3: 35.8 us, with such branches 41.6).  Rows past the last group are
-// left alone, and cost nothing but the end of a loop.
+// to e4m3: 34.7 us, with such branches 41).  Rows past the last group are left
+// alone, and cost no more than a wave that ends at once.
 //
-// Bound by HBM: those 16384 rows move 168 MB, 4.7 TB/s; 16396 rows of 2888 to
-// both types 63 us, 5.2 TB/s; the gradient of 4096 rows of 2048 to both types
-// 22.3 us, 4.5 TB/s.
+// Bound by HBM: those 16384 rows move 168 MB, 4.8 TB/s; 16396 rows of 2888 to
+// both types 60 us, 5.5 TB/s; the gradient of 4096 rows of 2048 to both types
+// 20.6 us, 4.9 TB/s.
 #include <algorithm>
 
 #include "block_common.h"
@@ -23,9 +25,7 @@ namespace nuna {
 namespace {
 
 constexpr int kNone = -1;
-constexpr int kBlocksPerWave = 8;
-constexpr int kSets = 2;                                  // of a wave's columns
-constexpr int kSetCols = kBlocksPerWave * kF8Block / kSets;  // 8 a lane
+constexpr int kBlocksPerWave = 64 * 8 / kF8Block;  // 8 columns a lane
 
 struct Outputs {
     char* out;
@@ -65,7 +65,7 @@ __device__ __forceinline__ int64_t used_rows(const SwigluArgs& a) {
     return a.offsets ? group_offset(a.offsets, a.groups, a.rows) : a.rows;
 }
 
-// f(row, first column of this lane's first eight) for every set of columns of the rows in use.
+// f(row, first of this lane's eight columns) for every set of columns of the rows in use.
 template <class F>
 __device__ __forceinline__ void for_items(int64_t rows, int chunks, F f) {
     const int64_t items = rows * chunks;
@@ -83,22 +83,13 @@ __global__ __launch_bounds__(kWG) void k_swiglu(SwigluArgs a, Outputs o, int chu
     constexpr int ES = Arith<DT>::kEsize;
     for_items(used_rows(a), chunks, [&](int64_t row, int64_t c) {
         const char* const p = static_cast<const char*>(a.gu) + row * 2 * a.inner * ES;
-        Raw8<DT> rg[kSets], ru[kSets];
+        const Raw8<DT> rg = load_raw8<DT, WHOLE>(p, c, a.inner), ru = load_raw8<DT, WHOLE>(p + a.inner * ES, c, a.inner);
+        float g[8], u[8];
+        widen<DT>(rg, c < a.inner, g);
+        widen<DT>(ru, c < a.inner, u);
 #pragma unroll
-        for (int s = 0; s < kSets; ++s) {
-            rg[s] = load_raw8<DT, WHOLE>(p, c + s * kSetCols, a.inner);
-            ru[s] = load_raw8<DT, WHOLE>(p + a.inner * ES, c + s * kSetCols, a.inner);
-        }
-#pragma unroll
-        for (int s = 0; s < kSets; ++s) {
-            const int64_t n = a.inner - c - s * kSetCols;
-            float g[8], u[8];
-            widen<DT>(rg[s], n > 0, g);
-            widen<DT>(ru[s], n > 0, u);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) g[i] = g[i] * sigmoid(g[i]) * u[i];
-            put<DT, KIND>(o, row, c + s * kSetCols, n, g);
-        }
+        for (int i = 0; i < 8; ++i) g[i] = g[i] * sigmoid(g[i]) * u[i];
+        put<DT, KIND>(o, row, c, a.inner - c, g);
     });
 }
 
@@ -115,30 +106,22 @@ __global__ __launch_bounds__(kWG) void k_swiglu_grad(SwigluArgs a, Outputs o, in
     for_items(used_rows(a), chunks, [&](int64_t row, int64_t c) {
         const char* const p = static_cast<const char*>(a.gu) + row * 2 * a.inner * ES;
         const char* const d = static_cast<const char*>(a.dout) + row * a.inner * ES;
-        Raw8<DT> rg[kSets], ru[kSets], rd[kSets];
+        const Raw8<DT> rg = load_raw8<DT, WHOLE>(p, c, a.inner), ru = load_raw8<DT, WHOLE>(p + a.inner * ES, c, a.inner);
+        const Raw8<DT> rd = load_raw8<DT, WHOLE>(d, c, a.inner);
+        const int64_t n = a.inner - c;
+        if (n <= 0) return;
+        float g[8], u[8], dh[8];
+        widen<DT>(rg, true, g);
+        widen<DT>(ru, true, u);
+        widen<DT>(rd, true, dh);
 #pragma unroll
-        for (int s = 0; s < kSets; ++s) {
-            rg[s] = load_raw8<DT, WHOLE>(p, c + s * kSetCols, a.inner);
-            ru[s] = load_raw8<DT, WHOLE>(p + a.inner * ES, c + s * kSetCols, a.inner);
-            rd[s] = load_raw8<DT, WHOLE>(d, c + s * kSetCols, a.inner);
-        }
-#pragma unroll
-        for (int s = 0; s < kSets; ++s) {
-            const int64_t at = c + s * kSetCols, n = a.inner - at;
-            if (n <= 0) continue;
-            float g[8], u[8], dh[8];
-            widen<DT>(rg[s], true, g);
-            widen<DT>(ru[s], true, u);
-            widen<DT>(rd[s], true, dh);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) gradients(g[i], u[i], dh[i], g[i], u[i]);
-            put<DT, KIND>(o, row, at, n, g);
-            put<DT, KIND>(o, row, a.inner + at, n, u);
-            if constexpr (KIND != kNone) {
-                // The entries of the scales past the last block, which no lane's columns reach.
-                if (at == 0)
-                    for (int64_t b = o.blocks; b < o.pitch; ++b) store_scale<KIND>(o.q_scale, row * o.pitch + b, kScaleOne<KIND>);
-            }
+        for (int i = 0; i < 8; ++i) gradients(g[i], u[i], dh[i], g[i], u[i]);
+        put<DT, KIND>(o, row, c, n, g);
+        put<DT, KIND>(o, row, a.inner + c, n, u);
+        if constexpr (KIND != kNone) {
+            // The entries of the scales past the last block, which no lane's columns reach.
+            if (c == 0)
+                for (int64_t b = o.blocks; b < o.pitch; ++b) store_scale<KIND>(o.q_scale, row * o.pitch + b, kScaleOne<KIND>);
         }
     });
 }
@@ -149,41 +132,37 @@ template <int DT, int KIND>
 __global__ __launch_bounds__(kWG) void k_swiglu_grad_across(SwigluArgs a, Outputs o, int chunks) {
     constexpr int ES = Arith<DT>::kEsize;
     using Raw = typename Arith<DT>::Raw;
-    for_items(used_rows(a), chunks, [&](int64_t row, int64_t c0) {
+    for_items(used_rows(a), chunks, [&](int64_t row, int64_t c) {
         const char* const gu = static_cast<const char*>(a.gu) + row * 2 * a.inner * ES;
         const char* const dout = static_cast<const char*>(a.dout) + row * a.inner * ES;
+        float v[8] = {};
+        if (c + 8 <= a.inner || c >= a.inner) {
+            const bool up_half = c >= a.inner;
+            const int64_t from = up_half ? c - a.inner : c, n = a.inner - from;
+            float g[8], u[8], dh[8];
+            load8<DT>(gu + from * ES, n, g);
+            load8<DT>(gu + (a.inner + from) * ES, n, u);
+            load8<DT>(dout + from * ES, n, dh);
 #pragma unroll
-        for (int s = 0; s < kSets; ++s) {
-            const int64_t c = c0 + s * kSetCols;
-            float v[8] = {};
-            if (c + 8 <= a.inner || c >= a.inner) {
-                const bool up_half = c >= a.inner;
-                const int64_t from = up_half ? c - a.inner : c, n = a.inner - from;
-                float g[8], u[8], dh[8];
-                load8<DT>(gu + from * ES, n, g);
-                load8<DT>(gu + (a.inner + from) * ES, n, u);
-                load8<DT>(dout + from * ES, n, dh);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float dg, du;
-                    gradients(g[i], u[i], dh[i], dg, du);
-                    v[i] = up_half ? du : dg;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const bool up_half = c + i >= a.inner;
-                    const int64_t j = up_half ? c + i - a.inner : c + i;
-                    if (j >= a.inner) continue;
-                    float dg, du;
-                    gradients(Arith<DT>::widen1(reinterpret_cast<const Raw*>(gu)[j]),
-                              Arith<DT>::widen1(reinterpret_cast<const Raw*>(gu)[a.inner + j]),
-                              Arith<DT>::widen1(reinterpret_cast<const Raw*>(dout)[j]), dg, du);
-                    v[i] = up_half ? du : dg;
-                }
+            for (int i = 0; i < 8; ++i) {
+                float dg, du;
+                gradients(g[i], u[i], dh[i], dg, du);
+                v[i] = up_half ? du : dg;
             }
-            put<DT, KIND>(o, row, c, 2 * a.inner - c, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool up_half = c + i >= a.inner;
+                const int64_t j = up_half ? c + i - a.inner : c + i;
+                if (j >= a.inner) continue;
+                float dg, du;
+                gradients(Arith<DT>::widen1(reinterpret_cast<const Raw*>(gu)[j]),
+                          Arith<DT>::widen1(reinterpret_cast<const Raw*>(gu)[a.inner + j]),
+                          Arith<DT>::widen1(reinterpret_cast<const Raw*>(dout)[j]), dg, du);
+                v[i] = up_half ? du : dg;
+            }
         }
+        put<DT, KIND>(o, row, c, 2 * a.inner - c, v);
     });
 }
 
