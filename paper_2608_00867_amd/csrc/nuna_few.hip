@@ -348,7 +348,8 @@ static_assert(kFewMaxWidth <= 64 * kWaves * kF8Block, "a lane for each of a wave
 
 // h: work item (reached expert, 16 columns).  The workgroup's waves split the blocks of x among them; a wave has its next
 // blocks under way, of the next item where this one has no more.  The weights of a block pass all YT tiles of 16 tokens
-// that can be at one expert.  h is kept as [slot][part][width], bf16, width = inner to whole blocks, zeros past inner.
+// that can be at one expert.  h is kept as [slot][part][width], bf16, width = inner to whole blocks; the last columns' items
+// write the zeros past inner.
 template <int DT, int KIND, int YT>
 __global__ __launch_bounds__(kWaves * 64, 2) void k_few_up(FewArgs a, uint16_t* __restrict__ h) {
     constexpr int S = kXParts<DT>, HS = kHParts<DT>;
@@ -366,7 +367,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_few_up(FewArgs a, uint16_t* 
     const int64_t width = f8_width(a.inner), kp = static_cast<int64_t>(blocks) * kF8Block;
     const int64_t pitch = (blocks + 3) / 4 * 4;
     const int64_t scale_rows = (2 * a.inner + kF8Block - 1) / kF8Block;
-    const int tiles = static_cast<int>(width / kTile), items = routing.count * tiles;
+    const int tiles = static_cast<int>((a.inner + kTile - 1) / kTile), items = routing.count * tiles;
     const int per = (blocks + kWaves - 1) / kWaves;
     const int kb0 = min(wave * per, blocks), kb1 = min(kb0 + per, blocks);
     const int64_t to_up = a.inner * kp;
@@ -534,6 +535,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_few_up(FewArgs a, uint16_t* 
 #pragma unroll
                 for (int p = 0; p < HS; ++p)
                     h[(static_cast<int64_t>(slots[t * kTile + y]) * HS + p) * width + c0 + c] = static_cast<uint16_t>(part[p]);
+            }
+            if (c0 + kTile >= a.inner) {
+                const int pad = static_cast<int>(width - c0 - kTile);
+                for (int o = tid; o < min(n - t * kTile, kTile) * HS * pad; o += kWaves * 64) {
+                    const int row = o / pad;
+                    h[(static_cast<int64_t>(slots[t * kTile + row / HS]) * HS + row % HS) * width + c0 + kTile + o % pad] = 0;
+                }
             }
         }
     }
@@ -726,7 +734,7 @@ hipError_t launch_expert_layer_few(const FewArgs& a, hipStream_t stream) {
     uint16_t* const h = static_cast<uint16_t*>(a.workspace);
     const int64_t experts = std::min<int64_t>(static_cast<int64_t>(a.tokens) * a.topk, a.experts);
     // A workgroup for each compute unit (two of them hold the registers of no more).
-    const int64_t up = std::min(std::min<int64_t>(experts * (f8_width(a.inner) / kTile), 256), grid_limit(256));
+    const int64_t up = std::min(std::min<int64_t>(experts * ((a.inner + kTile - 1) / kTile), 256), grid_limit(256));
     // 32 columns an item read h half as often as 16 (1 token, hidden 7168: 25 us, with 16 columns 33), but leave compute
     // units without work where there are fewer than about 200 (7 tokens, hidden 2880, fp32: the layer 88 us, with 16 82).
     const auto items = [&](int xt) { return (a.hidden + xt * kTile - 1) / (xt * kTile); };
