@@ -484,6 +484,20 @@ def test_few(nuna, T, k, E, first, count, H, inner, dtype, kind):
     assert torch.equal(nuna.expert_layer_few(x, dev(idx), w, *packed, first_expert=first), out)
 
 
+@pytest.mark.parametrize("inner", [1, 16, 65, 112, 129, 200, 1440])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [2, 23])
+def test_few_takes_a_workspace_of_nan(nuna, inner, dtype, T):
+    packed, _ = experts_of(nuna, 3, 136, inner, "f32", inner)
+    idx = dev(routing(T, 2, 3, inner))
+    x, w = values((T, 136), dtype, T)[0], torch.rand((T, 2), generator=torch.Generator().manual_seed(1)).cuda()
+    out = []
+    for byte in (0, 255):
+        ws = torch.full((nuna.expert_layer_few_workspace(T, 2, 136, inner),), byte, dtype=torch.uint8, device="cuda")
+        out.append(nuna.expert_layer_few(x, idx, w, *packed, workspace=ws))
+    assert bool(out[0].isfinite().all()) and torch.equal(*out)
+
+
 @pytest.mark.parametrize("H,inner,cap", [(128, 640, 3), (200, 200, 1), (1152, 256, 2), (2200, 128, 1), (640, 384, 5)])
 def test_few_workgroups_of_many_items(nuna, H, inner, cap):
     """Few workgroups, whose waves have one to three blocks of an item and load those of the next ones ahead."""
