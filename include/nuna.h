@@ -684,7 +684,8 @@ nuna_status_t nuna_swiglu_grad(const void* dout, const void* gu, const int32_t* 
                                hipStream_t stream);
 
 /*
- * A whole expert layer for a few tokens (a decode step), in two kernels:
+ * A whole expert layer for a few tokens (a decode step), in two kernels (three
+ * where hidden is narrow):
  *   out[t] = sum over j of weights[t][j] * W2[e] SwiGLU(W1[e] x[t]),  e = topk_idx[t][j]
  * over the entries with an expert in [first_expert, first_expert + num_experts);
  * a token with none gets zeros.  Every reached expert's weights are read once;

@@ -126,6 +126,7 @@ struct FewArgs {
     void* workspace;
     int kind, dtype;
 };
+// Activations of all slots, and behind them the partial sums of the second kernel where it splits the experts.
 size_t expert_layer_few_workspace(int tokens, int topk, int64_t hidden, int64_t inner);
 hipError_t launch_expert_layer_few(const FewArgs& a, hipStream_t stream);
 

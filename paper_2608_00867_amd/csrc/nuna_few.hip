@@ -547,11 +547,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_few_up(FewArgs a, uint16_t* 
     }
 }
 
-// out: work item 16 XT columns.  The reached experts' blocks of h follow each other in one line, of which every wave takes
+// out: work item (part, 16 XT columns).  The reached experts' blocks of h follow each other in one line, of which every wave takes
 // a run, its next blocks under way whichever experts they are of, and keeps sums of its own for every token; the
-// waves' are added in order.
+// waves' are added in order.  Where a layer has too few columns for the compute units the line is split in parts, whose
+// sums go to `partial` [parts][tokens][hidden] and are added by k_few_join (51 tokens, hidden 1440: the layer 262 us, in one
+// part 396).
 template <int DT, int KIND, int XT, int YT>
-__global__ __launch_bounds__(kWaves * 64, 2) void k_few_down(FewArgs a, const uint16_t* __restrict__ h) {
+__global__ __launch_bounds__(kWaves * 64, 2) void k_few_down(FewArgs a, const uint16_t* __restrict__ h, int parts,
+                                                             float* __restrict__ partial) {
     constexpr int HS = kHParts<DT>, kCols = XT * kTile;
     __shared__ Routing routing;
     __shared__ int tokens[kWaves][kFewTokens], slots[kWaves][kFewTokens];
@@ -568,11 +571,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_few_down(FewArgs a, const ui
     const int64_t scale_rows = (a.hidden + kF8Block - 1) / kF8Block;
     const int tiles = static_cast<int>((a.hidden + kCols - 1) / kCols);
     const int units = routing.count * blocks;
-    const int u0 = static_cast<int>(static_cast<int64_t>(units) * wave / kWaves);
-    const int u1 = static_cast<int>(static_cast<int64_t>(units) * (wave + 1) / kWaves);
     constexpr int kSS = KIND == kScaleF32 ? 4 : 1;
-    for (int item = blockIdx.x; item < tiles; item += gridDim.x) {
-        const int64_t c0 = static_cast<int64_t>(item) * kCols;
+    for (int item = blockIdx.x; item < tiles * parts; item += gridDim.x) {
+        const int part = item / tiles, run = part * kWaves + wave;
+        const int64_t c0 = static_cast<int64_t>(item - part * tiles) * kCols;
+        const int u0 = static_cast<int>(static_cast<int64_t>(units) * run / (kWaves * parts));
+        const int u1 = static_cast<int>(static_cast<int64_t>(units) * (run + 1) / (kWaves * parts));
         uint32_t row[2 * XT];  // this lane's parts of the rows, in a matrix of less than 2^32 bytes
 #pragma unroll
         for (int x = 0; x < 2 * XT; ++x)
@@ -716,18 +720,53 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_few_down(FewArgs a, const ui
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) v += sums[w * outputs + i];
             const int64_t t = i / kCols, c = c0 + i % kCols;
-            if (c < a.hidden) Arith<DT>::store1(a.out, t * a.hidden + c, v);
+            if (c >= a.hidden) continue;
+            if (parts == 1)
+                Arith<DT>::store1(a.out, t * a.hidden + c, v);
+            else
+                partial[(static_cast<int64_t>(part) * a.tokens + t) * a.hidden + c] = v;
         }
         meet();
     }
 }
 
+// out = the parts' sums, in order.
+template <int DT>
+__global__ __launch_bounds__(kWG) void k_few_join(const float* __restrict__ partial, int parts, int64_t n, void* __restrict__ out) {
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kWG + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * kWG) {
+        float v = partial[i];
+#pragma unroll 4
+        for (int p = 1; p < parts; ++p) v += partial[p * n + i];
+        Arith<DT>::store1(out, i, v);
+    }
+}
+
+// Columns of an item of the second kernel, in tiles: 32 read h half as often as 16 (1 token, hidden 7168: 25 us, with 16
+// columns 33), but leave compute units without work where there are fewer than about 200 items (7 tokens, hidden 2880, fp32:
+// the layer 88 us, with 16 82).
+int column_tiles(int tokens, int64_t hidden) { return tokens <= kTile && hidden < 192 * 2 * kTile ? 1 : 2; }
+int64_t column_items(int tokens, int64_t hidden) {
+    const int cols = column_tiles(tokens, hidden) * kTile;
+    return (hidden + cols - 1) / cols;
+}
+// Parts of the line of blocks: as many as fill the compute units, where less than half of them would have work.  (It does not
+// depend on how many workgroups run.)
+constexpr int kMostParts = 16;
+int parts_of(int tokens, int topk, int64_t hidden, int64_t inner) {
+    const int64_t items = column_items(tokens, hidden), units = static_cast<int64_t>(tokens) * topk * (f8_width(inner) / kF8Block);
+    if (items > 128) return 1;
+    // A wave of a part has a few blocks, if the tokens' experts differ.
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({256 / items, units / (4 * kWaves), kMostParts})));
+}
+size_t activations(int tokens, int topk, int64_t inner) {
+    return static_cast<size_t>(tokens) * topk * 3 * f8_width(inner) * sizeof(uint16_t);  // in three parts at most
+}
+
 }  // namespace
 
 size_t expert_layer_few_workspace(int tokens, int topk, int64_t hidden, int64_t inner) {
-    (void)hidden;
-    // h of every slot, in three parts at most.
-    return static_cast<size_t>(tokens) * topk * 3 * f8_width(inner) * sizeof(uint16_t);
+    const int parts = parts_of(tokens, topk, hidden, inner);
+    return activations(tokens, topk, inner) + (parts > 1 ? static_cast<size_t>(parts) * tokens * hidden * sizeof(float) : 0);
 }
 
 hipError_t launch_expert_layer_few(const FewArgs& a, hipStream_t stream) {
@@ -735,11 +774,9 @@ hipError_t launch_expert_layer_few(const FewArgs& a, hipStream_t stream) {
     const int64_t experts = std::min<int64_t>(static_cast<int64_t>(a.tokens) * a.topk, a.experts);
     // A workgroup for each compute unit (two of them hold the registers of no more).
     const int64_t up = std::min(std::min<int64_t>(experts * ((a.inner + kTile - 1) / kTile), 256), grid_limit(256));
-    // 32 columns an item read h half as often as 16 (1 token, hidden 7168: 25 us, with 16 columns 33), but leave compute
-    // units without work where there are fewer than about 200 (7 tokens, hidden 2880, fp32: the layer 88 us, with 16 82).
-    const auto items = [&](int xt) { return (a.hidden + xt * kTile - 1) / (xt * kTile); };
-    const int xt = a.tokens <= kTile && items(2) < 192 ? 1 : 2;
-    const int64_t down = std::min<int64_t>(items(xt), grid_limit(int64_t(1) << 20));
+    const int xt = column_tiles(a.tokens, a.hidden), parts = parts_of(a.tokens, a.topk, a.hidden, a.inner);
+    float* const partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + activations(a.tokens, a.topk, a.inner));
+    const int64_t down = std::min<int64_t>(column_items(a.tokens, a.hidden) * parts, grid_limit(int64_t(1) << 20));
     const size_t lds = static_cast<size_t>(kWaves) * a.tokens * xt * kTile * sizeof(float);
     using std::integral_constant;
     const auto run = [&](auto dt, auto kind, auto yt) {
@@ -747,15 +784,15 @@ hipError_t launch_expert_layer_few(const FewArgs& a, hipStream_t stream) {
         k_few_up<DT, KIND, YT><<<static_cast<uint32_t>(up), kWaves * 64, 0, stream>>>(a, h);
         note_launch("k_few_up", kMapLinear, 1, up, kWaves * 64, 1);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        if constexpr (YT == 1) {
-            if (xt == 1) {
-                k_few_down<DT, KIND, 1, YT><<<static_cast<uint32_t>(down), kWaves * 64, lds, stream>>>(a, h);
-                note_launch("k_few_down", kMapLinear, 1, down, kWaves * 64, 1);
-                return hipGetLastError();
-            }
-        }
-        k_few_down<DT, KIND, 2, YT><<<static_cast<uint32_t>(down), kWaves * 64, lds, stream>>>(a, h);
-        note_launch("k_few_down", kMapLinear, 1, down, kWaves * 64, 2);
+        if (YT == 1 && xt == 1)
+            k_few_down<DT, KIND, YT == 1 ? 1 : 2, YT><<<static_cast<uint32_t>(down), kWaves * 64, lds, stream>>>(a, h, parts, partial);
+        else
+            k_few_down<DT, KIND, 2, YT><<<static_cast<uint32_t>(down), kWaves * 64, lds, stream>>>(a, h, parts, partial);
+        note_launch("k_few_down", kMapLinear, 1, down, kWaves * 64, xt);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess || parts == 1) return e;
+        const int64_t n = a.tokens * a.hidden, join = std::min<int64_t>((n + kWG - 1) / kWG, grid_limit(int64_t(1) << 20));
+        k_few_join<DT><<<static_cast<uint32_t>(join), kWG, 0, stream>>>(partial, parts, n, a.out);
+        note_launch("k_few_join", kMapLinear, 1, join, kWG, 1);
         return hipGetLastError();
     };
     const auto sized = [&](auto dt, auto kind) {
