@@ -96,8 +96,17 @@ __device__ __forceinline__ float dpp_add(float v) {
     return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 
+template <int CTRL>
+__device__ __forceinline__ double dpp_add(double v) {
+    const int64_t b = __double_as_longlong(v);
+    const uint32_t lo = __builtin_amdgcn_mov_dpp(static_cast<int>(b), CTRL, 0xf, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_mov_dpp(static_cast<int>(b >> 32), CTRL, 0xf, 0xf, true);
+    return v + __longlong_as_double(static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo));
+}
+
 // Sum over each row of 16 lanes, the same in all of them: lanes one apart, two apart, four and eight (turned round).
-__device__ __forceinline__ float sum16(float v) {
+template <class T>
+__device__ __forceinline__ T sum16(T v) {
     return dpp_add<0x140>(dpp_add<0x141>(dpp_add<0x4e>(dpp_add<0xb1>(v))));
 }
 
@@ -110,12 +119,18 @@ __device__ __forceinline__ float lane_value(float v, int lane) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
 }
 
+__device__ __forceinline__ double lane_value(double v, int lane) {
+    const int64_t b = __double_as_longlong(v);
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(b), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(b >> 32), lane);
+    return __longlong_as_double(static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo));
+}
+
 // Sum over groups of P lanes (16, 32 or 64), the same in all lanes of a group.  All lanes of the wave take part.
-template <int P>
-__device__ __forceinline__ float sum_lanes(float v) {
+template <int P, class T>
+__device__ __forceinline__ T sum_lanes(T v) {
     v = sum16(v);
     if constexpr (P == 16) return v;
-    const float a = lane_value(v, 0) + lane_value(v, 16), b = lane_value(v, 32) + lane_value(v, 48);
+    const T a = lane_value(v, 0) + lane_value(v, 16), b = lane_value(v, 32) + lane_value(v, 48);
     if constexpr (P == 32) return (threadIdx.x & 32) ? b : a;
     return a + b;
 }
@@ -137,12 +152,13 @@ __device__ __forceinline__ float sigmoid(float g) {
 
 // Sum over the workgroup, the same in all threads.  `parts`: LDS for 16 waves' sums, which no earlier call may still be
 // read from.
-__device__ __forceinline__ float sum_workgroup(float v, float* parts) {
+template <class T>
+__device__ __forceinline__ T sum_workgroup(T v, T* parts) {
     v = sum_lanes<64>(v);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     if ((threadIdx.x & 63) == 0) parts[wave] = v;
     __syncthreads();
-    float s = parts[0];
+    T s = parts[0];
     for (int i = 1; i < waves; ++i) s += parts[i];
     return s;
 }
