@@ -21,7 +21,7 @@
 // Rates, of the weights' bytes alone.  One token, 8 experts of 7168 x 2048 (352
 // MB): 48.4 us for the first products, 4.9 TB/s, and 24.8 for the second, 4.7;
 // reads of the same lines with nothing else take 38.8 and 20.  64 tokens on 30
-// of 32 such experts: 160 and 71 us, 5.9 and 6.2 TB/s.
+// of 32 such experts: 160 to 164 and 71 us, 5.7 and 6.2 TB/s.
 #include <algorithm>
 
 #include "block_common.h"
