@@ -484,6 +484,21 @@ def test_few(nuna, T, k, E, first, count, H, inner, dtype, kind):
     assert torch.equal(nuna.expert_layer_few(x, dev(idx), w, *packed, first_expert=first), out)
 
 
+@pytest.mark.parametrize("T,k,E,H,inner", [(1, 8, 8, 128, 2048), (16, 8, 12, 96, 512), (11, 4, 12, 400, 384), (40, 8, 8, 300, 300),
+                                           (64, 4, 3, 17, 640), (30, 6, 7, 1440, 136)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_narrow_rows_are_summed_in_parts(nuna, T, k, E, H, inner, dtype):
+    k = min(k, E)
+    idx = routing(T, k, E, T + H, 0.1)
+    packed, plain = experts_of(nuna, E, H, inner, "e8m0", H + inner)
+    x, x64 = values((T, H), dtype, T, 0.3)
+    w = torch.randn((T, k), generator=torch.Generator().manual_seed(k)).cuda()
+    assert nuna.expert_layer_few_workspace(T, k, H, inner) > 6 * T * k * nuna.f8_width(inner)  # there are parts
+    out = check_few(nuna, x, x64, idx, w, packed, plain, 0, dtype)
+    nothing = nuna.expert_layer_few(x, dev(np.full_like(idx, -1)), w, *packed)
+    assert bool((nothing == 0).all()) and bool(out.isfinite().all())
+
+
 @pytest.mark.parametrize("inner", [1, 16, 65, 112, 129, 200, 1440])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T", [2, 23])
